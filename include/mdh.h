@@ -491,6 +491,100 @@ mdh_status mdh_matmul_ex(int64_t batch, int64_t M, int64_t N, int64_t K, const f
                          int32_t trans_c, const mdh_tile_params* params, void* workspace,
                          size_t workspace_bytes, void* stream);
 
+/* ------------------------------------------------------------------------- */
+/* Sequence layers: a prefix sum of matrices with decay, and group norm       */
+/* ------------------------------------------------------------------------- */
+
+/* Element types of the operands below (parameters, statistics and states are fp32). */
+typedef enum mdh_dtype { MDH_F32 = 0, MDH_BF16 = 1 } mdh_dtype;
+
+/*
+ * Linear attention with a decay for each head: the prefix-sum operator on matrices,
+ *   S_t = l S_{t-1} + k_t v_t^T      (dk x dv, l = exp(log_decay[h]))
+ *   o_t = scale * S_t^T q_t          for every batch entry b, token t < lengths[b] and head h,
+ * md_hom(k v^T, (++, ++, prefix-sum(op))) over (b, h, t) with (S1, n1) op (S2, n2) =
+ * (l^n2 S1 + S2, n1 + n2) (paper: Appendix, Example "Prefix-Sum"), whose combined value of the
+ * parts before a part is a matrix instead of mdh_scan's one number.
+ *   sizes    (B, T, H, Hq, Hk, Hv, dk, dv): H heads of decays, states and outputs; q, k and v have
+ *            Hq, Hk and Hv heads, which divide H: head h reads theirs number h / (H / Hq), ...
+ *            B, T >= 0, the others >= 1, dk and dv <= 256.
+ *   q, k, v  (B, T, Hq, dk), (B, T, Hk, dk), (B, T, Hv, dv); o: (B, T, H, dv); of type dtype
+ *   strides  12 numbers, (batch, token, head) of q, k, v, o in elements; channels are adjacent.
+ *            NULL: all dense.  Inputs may have stride 0 (one value for all).  Any alignment that the
+ *            type has; 16 bytes (base, strides and rows) are several times faster.
+ *   log_decay  H fp32, natural logarithm, <= 0; -infinity is l = 0
+ *   lengths  B int32 or NULL (all T).  Tokens from lengths[b] on are not read (any value, NaN too);
+ *            their outputs are 0.  Less than 0 counts as 0, more than T as T.
+ *   initial_state, final_state  (B, H, dk, dv) fp32, 16-byte aligned; NULL: zeros / not wanted.  They may
+ *            be the same buffer.  With slots (B int32) they are pools of n_slots states, and batch
+ *            entry b has that of slots[b]; outside of [0, n_slots) it has none: zeros, none written.
+ *            The slots of one call are distinct.
+ *   workspace  mdh_linattn_workspace_size(sizes, dtype, 0) bytes, 16-byte aligned (NULL where that is 0)
+ * Sums and states are fp32.  With fp32 operands every product is as exact as fp32's (three bf16 slices
+ * a value, six products); with bf16 operands scores and states are rounded to bf16 where they enter a
+ * product with v or q, the state itself is not.  Valid tokens hold finite values: one that is not may
+ * turn the outputs of up to 63 tokens before it, and of all behind it, into NaN.
+ */
+size_t mdh_linattn_workspace_size(const int64_t* sizes, mdh_dtype dtype, int32_t backward);
+mdh_status mdh_linattn(const int64_t* sizes, mdh_dtype dtype, const void* q, const void* k, const void* v,
+                       const int64_t* strides, const float* log_decay, float scale, const int32_t* lengths,
+                       const float* initial_state, float* final_state, const int32_t* slots, int64_t n_slots, void* o,
+                       void* workspace, size_t workspace_bytes, void* stream);
+
+/*
+ * Gradients of mdh_linattn.  With E_T = d_final_state and G_t = E_t + scale q_t do_t^T, E_{t-1} = l G_t:
+ *   dq_t = scale S_t do_t,   dk_t = G_t v_t,   dv_t = G_t^T k_t,   d_initial_state = E_0
+ * -- the forward pass over other operands, for dk and dv from the last token to the first.  Those of
+ * shared heads are summed in fp32 in a fixed order, and rounded once.
+ *   strides  21 numbers: (batch, token, head) of q, k, v, d_o, d_q, d_k, d_v; NULL: all dense
+ *   initial_state  what the forward call had; d_final_state, d_initial_state: NULL = zeros / not wanted; two buffers
+ *   workspace  mdh_linattn_workspace_size(sizes, dtype, 1) bytes
+ * The decay is a constant of the layer: it gets no gradient.
+ */
+mdh_status mdh_linattn_backward(const int64_t* sizes, mdh_dtype dtype, const void* q, const void* k, const void* v,
+                                const void* d_o, const int64_t* strides, const float* log_decay, float scale,
+                                const int32_t* lengths, const float* initial_state, const float* d_final_state, void* d_q,
+                                void* d_k, void* d_v, float* d_initial_state, void* workspace, size_t workspace_bytes,
+                                void* stream);
+
+/*
+ * One token of mdh_linattn with the state in place: state = l state + k v^T, o = scale state^T q.
+ *   sizes    (B, H, Hq, Hk, Hv, dk, dv);  q, k, v, o: (B, heads, channels)
+ *   strides  8 numbers, (batch, head) of q, k, v, o; NULL: all dense
+ *   state    (B, H, dk, dv) fp32, read and written; with slots a pool of n_slots of them, as above: a
+ *            batch entry without a slot has o = 0.  Pools may pass 2^31 elements.
+ */
+mdh_status mdh_linattn_step(const int64_t* sizes, mdh_dtype dtype, const void* q, const void* k, const void* v,
+                            const int64_t* strides, const float* log_decay, float scale, float* state,
+                            const int32_t* slots, int64_t n_slots, void* o, void* stream);
+
+/*
+ * Group norm with an activation, channels last: the channels of a group (C / G of them, adjacent) at all
+ * S positions of entry n have one mean and one variance,
+ *   z = (x - mean) * rstd * weight[c] + bias[c],  rstd = 1 / sqrt(variance + eps)
+ *   y = act(z),  or  y = z * act(gate)  where there is a gate
+ *   sizes    (N, S, C, G), G divides C.  S = 1: rows, as the heads of a token; S = H*W: mdh_mcc's images.
+ *            N or S = 0 is an empty call (mean and rstd stay as they are; gradients of weight and bias are 0).
+ *   x, gate, y  N*S rows of C elements of type dtype; row_strides: 3 numbers, elements from row to row
+ *            of x, gate, y (NULL: dense); weight, bias: C fp32, or NULL (1 and 0)
+ *   mean, rstd  N*G fp32 each, or NULL: what the backward call wants
+ * Variances are sums of squared differences from a mean (no squares of x are subtracted), in fp32.
+ * Inf or NaN in a group makes that group NaN and no other.  One value a group (variance 0) gives bias.
+ */
+enum { MDH_ACT_NONE = 0, MDH_ACT_RELU = 1, MDH_ACT_SILU = 2, MDH_ACT_GELU = 3 /* z Phi(z) */ };
+size_t mdh_group_norm_workspace_size(const int64_t* sizes, mdh_dtype dtype, int32_t backward);
+mdh_status mdh_group_norm(const int64_t* sizes, mdh_dtype dtype, const void* x, const void* gate, const int64_t* row_strides,
+                          const float* weight, const float* bias, float eps, int32_t act, void* y, float* mean, float* rstd,
+                          void* workspace, size_t workspace_bytes, void* stream);
+/*
+ * Gradients of mdh_group_norm; mean and rstd are its outputs.  row_strides: 5 numbers, of x, gate, d_y, d_x,
+ * d_gate.  d_weight, d_bias: C fp32 or NULL; summed over all rows in a fixed order.  relu's slope at 0 is 0.
+ */
+mdh_status mdh_group_norm_backward(const int64_t* sizes, mdh_dtype dtype, const void* x, const void* gate,
+                                   const void* d_y, const int64_t* row_strides, const float* weight, const float* bias,
+                                   const float* mean, const float* rstd, int32_t act, void* d_x, void* d_gate,
+                                   float* d_weight, float* d_bias, void* workspace, size_t workspace_bytes, void* stream);
+
 /*
  * Small per-workload tile-parameter search (paper: Section "Auto-Tuning", with
  * the search space shrunk to this library's kernel instantiations): runs every

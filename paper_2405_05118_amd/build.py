@@ -36,6 +36,10 @@ SOURCES = [
     "mdh_custom_reduce_bits.hip",
     "mdh_reduce.hip",
     "mdh_matmul_ex.hip",
+    "mdh_api_seq.hip",
+    "mdh_linattn.hip",
+    "mdh_linattn_step.hip",
+    "mdh_group_norm.hip",
 ]
 
 # packed-fp32 VALU instructions (v_pk_*_f32) are switched off on purpose: some of their forms have

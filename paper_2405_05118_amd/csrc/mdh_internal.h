@@ -281,6 +281,70 @@ mdh_status launch_prl_bits(int S, int64_t nA, int64_t nB, int nF, const int32_t*
 const int* prl_bits_gate(void* ws, int64_t nA, int S);
 mdh_status launch_prl_bits_finish(int S, int64_t nA, void* ws, int32_t* score, int32_t* index, hipStream_t st);
 
+// ---- linear attention with decay (mdh_linattn*.hip) ----
+
+// Index function (b, t, h, channel) -> p[b * sb + t * st + (h / group) * sh + channel]
+struct HeadView {
+  const void* p;
+  int64_t sb, st, sh;
+  int group;  // heads that share one (1: none)
+  int vec;    // 16-byte accesses: base, strides and rows are multiples of 16 bytes
+};
+
+// One pass over the tokens: position p of a sequence of n tokens is token p, or n-1-p where rev is set;
+//   out_p = scale_r * ( a_p^T (state of positions < p, decayed) + scale_u * sum_{j <= p, near} l^(p-j) (a_p.b_j) c_j ),
+//   state <- l state + scale_u b_p c_p^T                                  (da x dc)
+// A position reads the state l^(i+shift) of the way from where its run of positions began: forward (shift 1) the state
+// decays before a position adds to it, backward in time (shift 0) afterwards.
+struct LinattnPass {
+  HeadView a, b, c, out;
+  int da, dc;
+  int out_f32;         // out holds fp32 (summed over shared heads afterwards)
+  float scale_r, scale_u;
+  int rev, shift;
+  const float* s_in;   // (batch or slot, H, da, dc), or (.., dc, da) where s_in_t is set; null: zeros
+  int s_in_t;
+  float* s_out;        // the same, plain; null: not wanted
+};
+
+struct LinattnCall {
+  int64_t B, T;
+  int H;
+  const float* log_decay;
+  const int32_t* lengths;
+  const int32_t* slots;
+  int64_t n_slots;
+};
+
+mdh_status launch_linattn_pass(const LinattnCall& c, const LinattnPass* passes, int n, int dtype, hipStream_t st);
+// dst[.., h, ..] = sum of the heads h * group .. of src (fp32, dense B x T x H x d)
+mdh_status launch_linattn_share(const LinattnCall& c, const float* src, int d, const HeadView& dst, int heads, int dtype,
+                                hipStream_t st);
+mdh_status launch_linattn_step(const LinattnCall& c, const HeadView& q, const HeadView& k, const HeadView& v,
+                               const HeadView& o, int dk, int dv, float scale, float* state, int dtype, hipStream_t st);
+
+// ---- group norm, channels last (mdh_group_norm.hip) ----
+
+// Row r of C elements is at p + r * stride (elements); vec: 16-byte accesses
+struct RowView {
+  const void* p;
+  int64_t stride;
+  int vec;
+};
+struct GroupNormCall {
+  int64_t N, S;
+  int C, G, dtype, act;
+  RowView x, gate, y, dx, dgate;  // y: d_y in the backward call
+  const float *weight, *bias;
+  float eps;
+  float *mean, *rstd;  // outputs of the forward call, inputs of the backward call
+  float *dweight, *dbias;
+  void* ws;
+};
+size_t group_norm_workspace(const GroupNormCall& c, bool backward);
+mdh_status launch_group_norm(const GroupNormCall& c, hipStream_t st);
+mdh_status launch_group_norm_backward(const GroupNormCall& c, hipStream_t st);
+
 // The runtime's "last error" is sticky per thread and other users of the runtime in the same
 // process leave harmless codes there (an event query that is not ready yet, for instance):
 // clear it before a launch so that the status read after the launch is that launch's own.
