@@ -538,7 +538,7 @@ mdh_status mdh_linattn(const int64_t* sizes, mdh_dtype dtype, const void* q, con
  * shared heads are summed in fp32 in a fixed order, and rounded once.
  *   strides  21 numbers: (batch, token, head) of q, k, v, d_o, d_q, d_k, d_v; NULL: all dense
  *   initial_state  what the forward call had; d_final_state, d_initial_state: NULL = zeros / not wanted; two buffers
- *   workspace  mdh_linattn_workspace_size(sizes, dtype, 1) bytes
+ *   workspace  mdh_linattn_workspace_size(sizes, dtype, 1) bytes, which hold what the forward call wants too
  * The decay is a constant of the layer: it gets no gradient.
  */
 mdh_status mdh_linattn_backward(const int64_t* sizes, mdh_dtype dtype, const void* q, const void* k, const void* v,

@@ -41,7 +41,8 @@ HeadView view_of(const void* p, const int64_t* strides, const LinattnSizes& z, i
   if (z.T == 1) v.st = 0;
   if (heads == 1) v.sh = 0;
   const int unit = 16 / bytes;
-  v.vec = (uintptr_t)p % 16 == 0 && v.sb % unit == 0 && v.st % unit == 0 && v.sh % unit == 0 && d % unit == 0;
+  // (and 64 rows lie within the reach of 31 bits)
+  v.vec = v.st >= 0 && v.st < ((int64_t)1 << 31) / (80 * bytes) && (uintptr_t)p % 16 == 0 && v.sb % unit == 0 && v.st % unit == 0 && v.sh % unit == 0 && d % unit == 0;
   return v;
 }
 
@@ -59,9 +60,14 @@ size_t share_bytes(const LinattnSizes& z, int heads, int d) {
   return heads == z.H ? 0 : up16((size_t)z.B * (size_t)z.T * (size_t)z.H * (size_t)d * sizeof(float));
 }
 
-size_t linattn_need(const LinattnSizes& z, mdh_dtype, bool backward) {
-  if (!backward) return 0;
-  return share_bytes(z, z.Hq, z.dk) + share_bytes(z, z.Hk, z.dk) + share_bytes(z, z.Hv, z.dv);
+size_t segment_bytes(const LinattnSizes& z, mdh_dtype dtype, bool backward) {
+  return up16(linattn_segment_bytes(z.B, z.T, z.H, z.dk, z.dv, dtype, backward));
+}
+size_t linattn_need(const LinattnSizes& z, mdh_dtype dtype, bool backward) {
+  const size_t forward = segment_bytes(z, dtype, false);
+  if (!backward) return forward;
+  const size_t n = segment_bytes(z, dtype, true) + share_bytes(z, z.Hq, z.dk) + share_bytes(z, z.Hk, z.dk) + share_bytes(z, z.Hv, z.dv);
+  return n > forward ? n : forward;  // one workspace for both calls of a training step
 }
 
 LinattnCall call_of(const LinattnSizes& z, const float* log_decay, const int32_t* lengths, const int32_t* slots, int64_t n_slots) {
@@ -106,7 +112,16 @@ mdh_status mdh_linattn(const int64_t* sizes, mdh_dtype dtype, const void* q, con
   p.scale_r = scale, p.scale_u = 1.f;
   p.rev = 0, p.shift = 1;
   p.s_in = initial_state, p.s_out = final_state;
-  return launch_linattn_pass(call_of(z, log_decay, lengths, slots, n_slots), &p, 1, dtype, (hipStream_t)stream);
+  const LinattnCall c = call_of(z, log_decay, lengths, slots, n_slots);
+  int64_t len;
+  const int n = linattn_segments(z.B, z.T, z.H, z.dk, z.dv, dtype, false, &len);
+  float* const states[1] = {(float*)workspace};
+  const int turned[1] = {0};
+  if (n > 1) {
+    const mdh_status r = launch_linattn_segments(c, &p, 1, n, len, states, dtype, (hipStream_t)stream);
+    if (r != MDH_OK) return r;
+  }
+  return launch_linattn_pass(c, &p, 1, n, len, states, turned, dtype, (hipStream_t)stream);
 }
 
 mdh_status mdh_linattn_backward(const int64_t* sizes, mdh_dtype dtype, const void* q, const void* k, const void* v,
@@ -149,7 +164,7 @@ mdh_status mdh_linattn_backward(const int64_t* sizes, mdh_dtype dtype, const voi
   p[2].da = z.dk, p[2].dc = z.dv;
   p[2].scale_r = 1.f, p[2].scale_u = scale, p[2].rev = 1;
   p[2].s_in = d_final_state, p[2].s_out = d_initial_state;
-  char* ws = (char*)workspace;
+  char* ws = (char*)workspace + segment_bytes(z, dtype, true);
   for (int i = 0; i < 3; ++i) {
     p[i].out = grad[i];
     if (heads[i] == z.H) continue;
@@ -157,7 +172,21 @@ mdh_status mdh_linattn_backward(const int64_t* sizes, mdh_dtype dtype, const voi
     p[i].out_f32 = 1;
     ws += share_bytes(z, heads[i], p[i].dc);
   }
-  st = launch_linattn_pass(c, p, 3, dtype, (hipStream_t)stream);
+  int64_t len;
+  const int n = linattn_segments(z.B, z.T, z.H, z.dk, z.dv, dtype, true, &len);
+  // the states of the segments, as dk x dv: forward in time for d_q, backward for d_k and d_v
+  float* const two[2] = {(float*)workspace, (float*)workspace + (size_t)z.B * z.H * n * z.dk * z.dv};
+  float* const states[3] = {two[0], two[1], two[1]};
+  const int turned[3] = {1, 1, 0};
+  if (n > 1) {
+    LinattnPass sums[2] = {};
+    sums[0].b = vk, sums[0].c = vv, sums[0].scale_u = 1.f, sums[0].shift = 1, sums[0].s_in = initial_state;
+    sums[1].b = vq, sums[1].c = vo, sums[1].scale_u = scale, sums[1].rev = 1, sums[1].s_in = d_final_state;
+    for (LinattnPass& s : sums) s.a = s.b, s.da = z.dk, s.dc = z.dv;
+    st = launch_linattn_segments(c, sums, 2, n, len, two, dtype, (hipStream_t)stream);
+    if (st != MDH_OK) return st;
+  }
+  st = launch_linattn_pass(c, p, 3, n, len, states, turned, dtype, (hipStream_t)stream);
   for (int i = 0; i < 3 && st == MDH_OK; ++i)
     if (p[i].out_f32) st = launch_linattn_share(c, (const float*)p[i].out.p, p[i].dc, grad[i], heads[i], dtype, (hipStream_t)stream);
   return st;

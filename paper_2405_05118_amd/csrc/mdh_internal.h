@@ -316,7 +316,15 @@ struct LinattnCall {
   int64_t n_slots;
 };
 
-mdh_status launch_linattn_pass(const LinattnCall& c, const LinattnPass* passes, int n, int dtype, hipStream_t st);
+// Segments that the tokens of a call are cut into, and the positions of one (host rule); bytes of their states.
+int linattn_segments(int64_t B, int64_t T, int H, int dk, int dv, int dtype, bool backward, int64_t* len);
+size_t linattn_segment_bytes(int64_t B, int64_t T, int H, int dk, int dv, int dtype, bool backward);
+// states[i]: for pass i the state that enters each of n segments, (B, H, n, da, dc).  The passes are of one size.
+mdh_status launch_linattn_segments(const LinattnCall& c, const LinattnPass* passes, int np, int n, int64_t len, float* const* states,
+                                   int dtype, hipStream_t st);
+// the passes themselves; with n > 1 from states[i], which are (.., dc, da) of pass i where turned[i] is set
+mdh_status launch_linattn_pass(const LinattnCall& c, const LinattnPass* passes, int np, int n, int64_t len, float* const* states,
+                               const int* turned, int dtype, hipStream_t st);
 // dst[.., h, ..] = sum of the heads h * group .. of src (fp32, dense B x T x H x d)
 mdh_status launch_linattn_share(const LinattnCall& c, const float* src, int d, const HeadView& dst, int heads, int dtype,
                                 hipStream_t st);
