@@ -41,10 +41,12 @@ HeadView view_of(const void* p, const int64_t* strides, const LinattnSizes& z, i
   if (z.T == 1) v.st = 0;
   if (heads == 1) v.sh = 0;
   const int unit = 16 / bytes;
-  // (and 64 rows lie within the reach of 31 bits)
-  v.vec = v.st >= 0 && v.st < ((int64_t)1 << 31) / (80 * bytes) && (uintptr_t)p % 16 == 0 && v.sb % unit == 0 && v.st % unit == 0 && v.sh % unit == 0 && d % unit == 0;
+  v.vec = (uintptr_t)p % 16 == 0 && v.sb % unit == 0 && v.st % unit == 0 && v.sh % unit == 0 && d % unit == 0;
   return v;
 }
+
+// the rows of 64 consecutive tokens are addressed with 31 bits
+bool out_of_reach(const HeadView& v, int bytes) { return v.st < 0 || v.st > (((int64_t)1 << 31) - 4096) / 64 / bytes; }
 
 // an output whose elements share a place has no value
 bool overlaps(const HeadView& v, const LinattnSizes& z, int heads) {
@@ -108,6 +110,7 @@ mdh_status mdh_linattn(const int64_t* sizes, mdh_dtype dtype, const void* q, con
   p.c = view_of(v, sub(2), z, z.Hv, z.dv, e);
   p.out = view_of(o, sub(3), z, z.H, z.dv, e);
   if (overlaps(p.out, z, z.H)) return MDH_ERR_SIZE;
+  if (out_of_reach(p.a, e) || out_of_reach(p.b, e) || out_of_reach(p.c, e) || out_of_reach(p.out, e)) return MDH_ERR_SIZE;
   p.da = z.dk, p.dc = z.dv;
   p.scale_r = scale, p.scale_u = 1.f;
   p.rev = 0, p.shift = 1;
@@ -149,7 +152,8 @@ mdh_status mdh_linattn_backward(const int64_t* sizes, mdh_dtype dtype, const voi
   const HeadView grad[3] = {view(4, z.Hq, z.dk), view(5, z.Hk, z.dk), view(6, z.Hv, z.dv)};
   const int heads[3] = {z.Hq, z.Hk, z.Hv};
   for (int i = 0; i < 3; ++i)
-    if (overlaps(grad[i], z, heads[i])) return MDH_ERR_SIZE;
+    if (overlaps(grad[i], z, heads[i]) || out_of_reach(grad[i], e)) return MDH_ERR_SIZE;
+  if (out_of_reach(vq, e) || out_of_reach(vk, e) || out_of_reach(vv, e) || out_of_reach(vo, e)) return MDH_ERR_SIZE;
   const LinattnCall c = call_of(z, log_decay, lengths, nullptr, 0);
   LinattnPass p[3] = {};
   p[0].a = vo, p[0].b = vv, p[0].c = vk;  // d_q: the forward state, from its other side

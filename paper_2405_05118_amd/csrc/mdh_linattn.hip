@@ -6,16 +6,16 @@
 // before the run; i, j positions in it):
 //   out = scale_r ( l^(i+shift) a_i^T S + scale_u sum_{j<=i} l^(i-j) (a_i.b_j) c_j ),   S <- l^n S + scale_u sum_j l^(..) b_j c_j^T
 // De-composition: (b, h), 64 or 128 columns of c and, with few of those, segments of the tokens go to workgroups; runs are
-// walked in order, S in registers: a wavefront owns 16 columns of it, all rows.  Scores a_i.b_j are divided over
+// walked in order, S in registers: a wavefront owns 16 or 32 columns of it, all rows.  Scores a_i.b_j are divided over
 // the wavefronts and exchanged through LDS.  Segments: a pass that only sums up states (reads b and c), a prefix sum over
 // the segments, then the pass itself, every segment from its state.
 //
 // Operands of the 16 x 16 x 32 block are read from LDS rows of a and b as they are, and through transposing reads of b and c
-// (ds_read_b64_tr_b16: a lane gets one column of four rows).  Rows and columns of S are dealt out so that the lane that
-// holds 4 rows of two blocks holds 8 consecutive ones: S is an operand of a_i^T S without leaving its registers.
+// (ds_read_b64_tr_b16: a lane gets one column of four rows).  S is an operand of a_i^T S without leaving its registers: of
+// 32 rows a lane has 4 of each 16, and reads the same channels of a, which lie side by side in LDS for that.
 //
-// fp32 operands are three bf16 slices each (24 bits, cut off: exact), and products the six largest of nine (2^-23 of a
-// product is lost).  bf16 operands are one slice; scores and S are rounded to one slice where they are operands (2^-9 of a
+// fp32 operands are three bf16 slices each (24 bits, cut off), and products the six largest of nine (2^-23 of a product is
+// lost).  bf16 operands are one slice; scores and S are rounded to one slice where they are operands (2^-9 of a
 // term, as the output's own rounding), but what is added to S is not: c_j times its decay is three slices.
 #include "mdh_internal.h"
 #include "mdh_types.h"
@@ -30,6 +30,9 @@ typedef uint32_t u4 __attribute__((ext_vector_type(4)));
 typedef uint32_t u2 __attribute__((ext_vector_type(2)));
 typedef __attribute__((address_space(3))) uint16_t Lds;
 typedef __attribute__((address_space(3))) u4 LdsU4;
+typedef __attribute__((address_space(3))) u2 LdsU2;
+typedef __attribute__((address_space(3))) float LdsF;
+typedef __attribute__((address_space(3))) f4 LdsF4;
 typedef __attribute__((address_space(3))) s4 LdsS4;
 
 __device__ __forceinline__ int64_t slot_of(const LinattnCall& c, int64_t b) {
@@ -47,9 +50,7 @@ struct Frag {
   u4 s[NS];
 };
 
-// the upper halves of two words
-__device__ __forceinline__ uint32_t upper(uint32_t lo, uint32_t hi) { return __builtin_amdgcn_perm(hi, lo, 0x07060302u); }
-
+// Two values in NS bf16 slices: one is rounded to nearest, three are cut off and hold all 24 bits.
 template <int NS, int N>
 __device__ __forceinline__ void split(const float (&x)[N], uint32_t (&out)[NS][N / 2]) {
 #pragma unroll
@@ -57,13 +58,13 @@ __device__ __forceinline__ void split(const float (&x)[N], uint32_t (&out)[NS][N
     if constexpr (NS == 1) {
       out[0][i / 2] = pack_bf16(x[i], x[i + 1]);
     } else {
-      float r0 = x[i], r1 = x[i + 1];
+      uint32_t r0 = __float_as_uint(x[i]), r1 = __float_as_uint(x[i + 1]);
 #pragma unroll
       for (int s = 0; s < NS; ++s) {
-        out[s][i / 2] = upper(__float_as_uint(r0), __float_as_uint(r1));
+        out[s][i / 2] = __builtin_amdgcn_perm(r1, r0, 0x07060302u);  // the upper halves
         if (s + 1 < NS) {
-          r0 -= __uint_as_float(__float_as_uint(r0) & 0xffff0000u);
-          r1 -= __uint_as_float(__float_as_uint(r1) & 0xffff0000u);
+          r0 = __float_as_uint(__uint_as_float(r0) - __uint_as_float(r0 & 0xffff0000u));
+          r1 = __float_as_uint(__uint_as_float(r1) - __uint_as_float(r1 & 0xffff0000u));
         }
       }
     }
@@ -107,98 +108,123 @@ __device__ __forceinline__ f4 mma(const Frag<NA>& a, const Frag<NB>& b, f4 acc) 
   return acc;
 }
 
-// 8 consecutive channels of a row as they come from memory.  load: through a descriptor whose loads past its 2^31 bytes give
-// 0, at byte `at` + `step`; parts that are not there are asked for past the end.  load_each: element by element, any
-// alignment and distance.
+// 8 consecutive channels of a row as they come from memory, at byte `at` + `step` of a descriptor whose loads past its 2^31
+// bytes give 0: parts that are not there are asked for past the end.  VEC: 16 bytes at a time, else element by element
+// (any alignment).
+constexpr int kWaves = 4, kThreads = 64 * kWaves;
 constexpr int kPast = (int)0x80000000;
 __device__ __forceinline__ __amdgpu_buffer_rsrc_t rsrc_of(const void* p) {
   return __builtin_amdgcn_make_buffer_rsrc(const_cast<void*>(p), 0, 0x7fffffff, 0x00027000);
 }
+// LOADS of them for 8 channels; each has its own place, past the end where its channels are not there.
 template <typename T>
-struct Raw;
-template <>
-struct Raw<bf16> {
-  u4 w;
-  __device__ __forceinline__ void load(__amdgpu_buffer_rsrc_t from, int at, int step, int col, int d, bool ok) {
-    w = __builtin_amdgcn_raw_buffer_load_b128(from, ok && col < d ? at : kPast, step, 0);
-  }
-  __device__ __forceinline__ void load_each(const bf16* row, int col, int d, bool ok) {
-    w = (u4){0, 0, 0, 0};
+struct Raw {
+  static constexpr int kLoads = sizeof(T) / 2, kPer = 16 / sizeof(T);  // 16-byte loads of a piece, channels of one
+  u4 w[kLoads];
+  __device__ __forceinline__ void load(__amdgpu_buffer_rsrc_t from, const int (&at)[kLoads], int step) {
 #pragma unroll
-    for (int e = 0; e < 8; ++e)
-      if (ok && col + e < d) w[e / 2] |= (uint32_t)row[col + e].bits << (16 * (e & 1));
+    for (int i = 0; i < kLoads; ++i) w[i] = __builtin_amdgcn_raw_buffer_load_b128(from, at[i], step, 0);
   }
-};
-template <>
-struct Raw<float> {
-  u4 w[2];
-  __device__ __forceinline__ void load(__amdgpu_buffer_rsrc_t from, int at, int step, int col, int d, bool ok) {
-    w[0] = __builtin_amdgcn_raw_buffer_load_b128(from, ok && col < d ? at : kPast, step, 0);
-    w[1] = __builtin_amdgcn_raw_buffer_load_b128(from, ok && col + 4 < d ? at + 16 : kPast, step, 0);
-  }
-  __device__ __forceinline__ void load_each(const float* row, int col, int d, bool ok) {
-    w[0] = w[1] = (u4){0, 0, 0, 0};
+  __device__ __forceinline__ void load_each(__amdgpu_buffer_rsrc_t from, int at, int step, int d) {
+    if constexpr (sizeof(T) == 2) {
 #pragma unroll
-    for (int e = 0; e < 8; ++e)
-      if (ok && col + e < d) w[e / 4][e & 3] = __float_as_uint(row[col + e]);
+      for (int e = 0; e < 4; ++e) {
+        const uint32_t lo = __builtin_amdgcn_raw_buffer_load_b16(from, 2 * e < d ? at + 4 * e : kPast, step, 0);
+        const uint32_t hi = __builtin_amdgcn_raw_buffer_load_b16(from, 2 * e + 1 < d ? at + 4 * e + 2 : kPast, step, 0);
+        w[0][e] = (lo & 0xffffu) | hi << 16;
+      }
+    } else {
+#pragma unroll
+      for (int e = 0; e < 8; ++e) w[e / 4][e & 3] = __builtin_amdgcn_raw_buffer_load_b32(from, e < d ? at + 4 * e : kPast, step, 0);
+    }
   }
 };
 
-// The rows of one operand that a run reads: lane i has channels col.. of rows row0, row0 + kStep, ..
-template <typename T, int C, int WIDE, int THREADS>
+// The rows of one operand that a run reads: the lane has channels col.. of positions row, row + kStep, .. of it
+template <typename T, int C, int WIDE>
 struct Rows {
-  static constexpr int kAcross = WIDE / 8, kStep = THREADS / kAcross, kPieces = C * kAcross, N = kPieces < THREADS ? 1 : kPieces / THREADS;
+  static constexpr int kAcross = WIDE / 8, kStep = kThreads / kAcross, N = C / kStep;
+  static_assert(C % kStep == 0 && N >= 1, "every lane has whole rows");
   Raw<T> r[N];
+  int at[Raw<T>::kLoads], pitch, rev;
+  const T* base;  // position 0's row would be here, were all runs full
+  int64_t st;
   static __device__ __forceinline__ int col() { return threadIdx.x % kAcross * 8; }
-  static __device__ __forceinline__ int row(int j) { return threadIdx.x / kAcross + j * kStep; }
-  // first: the run's lowest token; n of C rows are there, d channels of them
-  __device__ __forceinline__ void load(const HeadView& v, const T* first, int n, int d) {
-    if (v.vec) {
-      const int pitch = (int)(v.st * sizeof(T));
-      const __amdgpu_buffer_rsrc_t from = rsrc_of(first);
-      const int at = row(0) * pitch + col() * (int)sizeof(T);
+  static __device__ __forceinline__ int row() { return threadIdx.x / kAcross; }
+  __device__ __forceinline__ void init(const HeadView& v, int64_t offset, int d, int rev_) {
+    base = (const T*)v.p + offset;
+    st = v.st;
+    pitch = (int)(v.st * sizeof(T));
+    rev = rev_;
+    const int first = (rev ? C - 1 - row() - (N - 1) * kStep : row()) * pitch + col() * (int)sizeof(T);
 #pragma unroll
-      for (int j = 0; j < N; ++j) r[j].load(from, at, j * kStep * pitch, col(), d, row(j) < n);
-    } else {
-#pragma unroll
-      for (int j = 0; j < N; ++j) r[j].load_each(first + row(j) * v.st, col(), d, row(j) < n);
-    }
+    for (int i = 0; i < Raw<T>::kLoads; ++i) at[i] = col() + i * Raw<T>::kPer < d ? first + 16 * i : kPast;
   }
-  // to rows of LDS, the last token first where rev is set
-  template <int NS, int PITCH>
-  __device__ __forceinline__ void store(uint16_t* to, int n, int rev) const {
-    if (kPieces < THREADS && (int)threadIdx.x >= kPieces) return;
+  // the run of n positions whose first is pos, of len (all loads of a sequence's last run, which may be shorter, are checked)
+  __device__ __forceinline__ void load(int vec, int pos, int n, int len, int d) {
+    const __amdgpu_buffer_rsrc_t from = rsrc_of(base + (int64_t)(rev ? len - pos - C : pos) * st);
 #pragma unroll
     for (int j = 0; j < N; ++j) {
-      const int i = row(j);
-      uint16_t* at = to + (rev && i < n ? n - 1 - i : i) * PITCH + col();
+      const int step = (rev ? N - 1 - j : j) * kStep * pitch;
+      if (vec && n == C) {
+        r[j].load(from, at, step);
+      } else if (vec) {
+        int checked[Raw<T>::kLoads];
+#pragma unroll
+        for (int i = 0; i < Raw<T>::kLoads; ++i) checked[i] = row() + j * kStep < n ? at[i] : kPast;
+        r[j].load(from, checked, step);
+      } else {
+        const int first = (rev ? C - 1 - row() - (N - 1) * kStep : row()) * pitch + col() * (int)sizeof(T);
+        r[j].load_each(from, first, step, row() + j * kStep < n ? d - col() : 0);
+      }
+    }
+  }
+  // PAIRED: of 32 channels, 4g.. and 16 + 4g.. side by side
+  template <int NS, int PITCH, bool PAIRED = false>
+  __device__ __forceinline__ void store(Lds* to) const {
+    const int c = PAIRED ? (col() & ~31) + ((col() & 8) << 1) + ((col() & 16) >> 2) : col();
+    Lds* const first = to + row() * PITCH + c;
+#pragma unroll
+    for (int j = 0; j < N; ++j) {
+      Frag<NS> f;
       if constexpr (NS == 1) {
-        *(u4*)at = r[j].w;
+        f.s[0] = r[j].w[0];
       } else {
         float x[8];
 #pragma unroll
         for (int e = 0; e < 8; ++e) x[e] = __uint_as_float(r[j].w[e / 4][e & 3]);
-        const Frag<NS> f = frag_of<NS>(x);
+        f = frag_of<NS>(x);
+      }
 #pragma unroll
-        for (int s = 0; s < NS; ++s) *(u4*)(at + s * C * PITCH) = f.s[s];
+      for (int s = 0; s < NS; ++s) {
+        Lds* const to_s = first + (s * C + j * kStep) * PITCH;
+        if constexpr (PAIRED) {
+          *(LdsU2*)to_s = (u2){f.s[s][0], f.s[s][1]};
+          *(LdsU2*)(to_s + 8) = (u2){f.s[s][2], f.s[s][3]};
+        } else {
+          *(LdsU4*)to_s = f.s[s];
+        }
       }
     }
   }
 };
 
-// The shape of a kernel: KP rows of the state (da padded), W wavefronts with 16 columns each
-template <typename T, int KP_, int W_, bool STATE_>
+// The shape of a kernel: KP rows of the state (da padded), four wavefronts with NB blocks of 16 columns each.  Two blocks where
+// they can be: what a wavefront reads of a, b and the scores serves both, and LDS is what the passes are short of.
+template <typename T, int KP_, int NB_, bool STATE_>
 struct Shape {
   static constexpr int NS = sizeof(T) == 2 ? 1 : 3;
   static constexpr int C = NS == 1 ? 64 : 32;  // positions of a run
-  static constexpr int KP = KP_, W = W_, VT = 16 * W_;
+  static constexpr int KP = KP_, NB = NB_, VT = 16 * NB_ * kWaves;
   static constexpr bool STATE = STATE_;  // sums up the state only
   static constexpr int TB = C / 16, KS = KP / 32, CS = C / 32;
-  // rows in LDS, in elements: 16 bytes past a multiple of 128 bytes, so that 16 rows at one column are all banks
-  static constexpr int PA = KP + 8, PC = VT + 8, PP = C + 8;
-  static constexpr int A = 0, B = A + (STATE ? 0 : NS * C * PA), CC = B + NS * C * PA, P = CC + NS * C * PC;
+  // Rows in LDS, in elements, without bank conflicts.  a and scores are read 16 rows at a time at one column: 16 bytes past a
+  // multiple of 128 bytes.  A transposing read of b, or of c for two blocks, takes from 4 rows every other 8 bytes of 64:
+  // 64 bytes past a multiple of 256 (or short of it), so that the rows lie beside one another.
+  static constexpr int PA = KP + 8, PB = KP + 32, PC = NB == 2 ? VT + 32 : VT + 16, PP = C + 8;
+  static constexpr int A = 0, B = A + (STATE ? 0 : NS * C * PA), CC = B + NS * C * PB, P = CC + NS * C * PC;
   static constexpr int kHalves = P + (STATE ? 0 : NS * C * PP);
-  static constexpr int kBytes = kHalves * 2 + (C + 2 * (C + 4)) * 4;  // and the decays: l^(..) of an update, l^i
+  static constexpr int kBytes = kHalves * 2 + (5 * C + 4) * 4;  // and the decays (below)
 };
 
 struct SegmentArgs {
@@ -210,24 +236,25 @@ struct SegmentArgs {
 struct PassArgs {
   LinattnCall c;
   LinattnPass p[3];
-  int tiles[3];     // column tiles of each pass, of 16 W columns
+  int tiles[3];     // column tiles of each pass, of 64 NB columns
   int n;
   SegmentArgs seg[3];
   int seg_t[3];     // the states are (dc, da) of this pass
 };
 
-template <typename T, int KP, int W, bool STATE>
-__global__ __launch_bounds__(64 * W, KP == 256 ? 2 : KP == 128 && W == 4 ? 3 : 4) void linattn_runs_kernel(PassArgs args) {
-  using X = Shape<T, KP, W, STATE>;
-  constexpr int C = X::C, NS = X::NS, TB = X::TB, KS = X::KS, CS = X::CS, TH = 64 * W;
+template <typename T, int KP, int NB, bool STATE>
+__global__ __launch_bounds__(kThreads, 2) void linattn_runs_kernel(PassArgs args) {
+  using X = Shape<T, KP, NB, STATE>;
+  constexpr int C = X::C, NS = X::NS, TB = X::TB, KS = X::KS, CS = X::CS, TH = kThreads;
   extern __shared__ __align__(16) uint16_t lds[];
-  uint16_t* const As = lds + X::A;
-  uint16_t* const Bs = lds + X::B;
-  uint16_t* const Cs = lds + X::CC;
-  uint16_t* const Ps = lds + X::P;
-  float* const uw = (float*)(lds + X::kHalves);  // what position j of a run is multiplied with on its way into the state
-  float* const pw = uw + C;                      // l^i, i <= C, as two floats
-  float* const pl = pw + C + 4;
+  Lds* const As = (Lds*)lds + X::A;
+  Lds* const Bs = (Lds*)lds + X::B;
+  Lds* const Cs = (Lds*)lds + X::CC;
+  Lds* const Ps = (Lds*)lds + X::P;
+  LdsF* const uw = (LdsF*)((Lds*)lds + X::kHalves);  // what position j of a run is multiplied with on its way into the state,
+  LdsF* const fw = uw + C;                           // what position i reads of the state before the run,
+  LdsF* const nw = fw + 2 * C;                       // what position i reads of position i - d, 0 for d < 0
+  LdsF* const pw = nw + C;                           // and l^i, i <= C
 
   const LinattnCall& call = args.c;
   const int tid = threadIdx.x, lane = tid & 63, l16 = lane & 15, g = lane >> 4;
@@ -253,10 +280,12 @@ __global__ __launch_bounds__(64 * W, KP == 256 ? 2 : KP == 128 && W == 4 ? 3 : 4
   const int64_t slot = slot_of(call, b);
   const int64_t elems = (int64_t)da * dc, at = (slot * call.H + h) * elems;
   const int64_t seg_at = (((int64_t)b * call.H + h) * sg.n + seg) * elems;
-  const int tile0 = tile * X::VT, my_col = tile0 + 16 * wave + l16;  // of the state; of an output, a lane has rows of l16
+  const int tile0 = tile * X::VT, wave0 = 16 * NB * wave;  // first column of the tile, and in it of the wavefront
+  // the column of lane m in block nb: with two blocks every other four, so that an output's lane has 8 side by side
+  auto col_of = [&](int m, int nb) { return tile0 + wave0 + (NB == 2 ? 8 * (m >> 2) + 4 * nb + (m & 3) : m); };
 
-  // S[ks][x][r]: row 32 ks + 8 g + 4 x + r, column my_col
-  f4 S[KS][2];
+  // S[ks][x][nb][r]: row 32 ks + 16 x + 4 g + r, column col_of(l16, nb)
+  f4 S[KS][2][NB];
   {
     const float* from = nullptr;
     int turned = 0;
@@ -269,18 +298,20 @@ __global__ __launch_bounds__(64 * W, KP == 256 ? 2 : KP == 128 && W == 4 ? 3 : 4
         turned = p.s_in_t;
       }
     }
-const int down = turned ? 4 : dc * 4, lane_at = 8 * g * down + my_col * (turned ? da * 4 : 4);
-    const bool mine = from && my_col < dc;
-    const int rows_here = da - 8 * g;
+    const int down = turned ? 4 : dc * 4, across = turned ? da * 4 : 4, rows_here = da - 4 * g;
 #pragma unroll
     for (int ks = 0; ks < KS; ++ks)
 #pragma unroll
       for (int x = 0; x < 2; ++x)
 #pragma unroll
-        for (int r = 0; r < 4; ++r) {
-          const int row = 32 * ks + 4 * x + r;
-          S[ks][x][r] = __uint_as_float(
-              __builtin_amdgcn_raw_buffer_load_b32(rsrc_of(from), mine && row < rows_here ? lane_at : kPast, row * down, 0));
+        for (int nb = 0; nb < NB; ++nb) {
+          const int col = col_of(l16, nb), lane_at = 4 * g * down + col * across;
+#pragma unroll
+          for (int r = 0; r < 4; ++r) {
+            const int row = 32 * ks + 16 * x + r;
+            S[ks][x][nb][r] = __uint_as_float(__builtin_amdgcn_raw_buffer_load_b32(
+                rsrc_of(from), from && col < dc && row < rows_here ? lane_at : kPast, row * down, 0));
+          }
         }
   }
 
@@ -288,49 +319,52 @@ const int down = turned ? 4 : dc * 4, lane_at = 8 * g * down + my_col * (turned 
   auto update_weights = [&](int n) {  // of a run of n positions
     if (tid < C) uw[tid] = tid < n ? p.scale_u * pw[n - tid - p.shift] : 0.f;
   };
-  if (tid <= C) {
-    const Decay d = decay_power(log_decay, tid);
-    pw[tid] = d.hi;
-    pl[tid] = d.lo;
-  }
+  if (tid <= C) pw[tid] = decay_power(log_decay, tid).hi;
   __syncthreads();
   update_weights(C);
-  // score blocks of a wavefront: 16 rows tb, 16 columns sb0 ..; the upper half of the blocks is of no use to anybody
-  constexpr int BPW = TB * TB >= W ? TB * TB / W : 1;
-  const int tb = wave * BPW / TB, sb0 = wave * BPW % TB;
-  float near[BPW][4], far[TB];
-  if (!STATE) {
-#pragma unroll
-    for (int i = 0; i < BPW; ++i)
-#pragma unroll
-      for (int r = 0; r < 4; ++r) {
-        const int d = 16 * (tb - sb0 - i) + l16 - 4 * g - r;
-        near[i][r] = d >= 0 && d <= C ? p.scale_r * p.scale_u * pw[d] : 0.f;
-      }
-#pragma unroll
-    for (int i = 0; i < TB; ++i) far[i] = p.scale_r * pw[16 * i + l16 + p.shift];
+  if (tid < C) {
+    fw[tid] = p.scale_r * pw[tid + p.shift];
+    nw[tid] = p.scale_r * p.scale_u * pw[tid];
+    nw[tid - C] = 0.f;
   }
+  // The state is multiplied with l^C run after run, by one float for each: the relative error that the roundings so far have
+  // left (`off`) is taken back by the next one.  Without that, 2^-25 a run adds up over a long memory.
+  const double run_decay = log_decay == 0.f ? 1.0 : exp((double)log_decay * C), per = run_decay > 0.0 ? 1.0 / run_decay : 0.0;
+  double off = 0.0;
+  // score blocks of a wavefront: 16 rows wave_tb, 16 columns sb0 ..; the upper half of the blocks is of no use to anybody
+  constexpr int BPW = TB * TB / kWaves;
+  const int wave_tb = wave * BPW / TB, sb0 = wave * BPW % TB;
 
   // operands: the rows of the next run, in registers until this one is done
-  Rows<T, C, KP, TH> ra, rb;
-  Rows<T, C, X::VT, TH> rc;
-  const T* const pa = (const T*)p.a.p + b * p.a.sb + (h / p.a.group) * p.a.sh;
-  const T* const pb = (const T*)p.b.p + b * p.b.sb + (h / p.b.group) * p.b.sh;
-  const T* const pc = (const T*)p.c.p + b * p.c.sb + (h / p.c.group) * p.c.sh + tile0;
+  Rows<T, C, KP> ra, rb;
+  Rows<T, C, X::VT> rc;
+  if (!STATE) ra.init(p.a, b * p.a.sb + (h / p.a.group) * p.a.sh, da, rev);
+  rb.init(p.b, b * p.b.sb + (h / p.b.group) * p.b.sh, da, rev);
+  rc.init(p.c, b * p.c.sb + (h / p.c.group) * p.c.sh + tile0, dc - tile0, rev);
   auto load = [&](int pos) {
     const int n = min(C, len - pos);
-    const int64_t t = rev ? len - pos - n : pos;
-    if (!STATE) ra.load(p.a, pa + t * p.a.st, n, da);
-    rb.load(p.b, pb + t * p.b.st, n, da);
-    rc.load(p.c, pc + t * p.c.st, n, dc - tile0);
+    if (!STATE) ra.load(p.a.vec, pos, n, len, da);
+    rb.load(p.b.vec, pos, n, len, da);
+    rc.load(p.c.vec, pos, n, len, dc - tile0);
   };
+  auto store = [&](int pos) {
+    if (!STATE) ra.template store<NS, X::PA, true>(As);
+    rb.template store<NS, X::PB, true>(Bs);
+    rc.template store<NS, X::PC>(Cs);
+    if (len - pos < C) update_weights(len - pos);
+  };
+  // outputs: a lane has 4 NB consecutive columns of position l16 of each block of 16
+  const int out_bytes = p.out_f32 ? 4 : (int)sizeof(T), out_pitch = (int)(p.out.st * out_bytes);
+  const int out_col = tile0 + wave0 + 4 * NB * g, out_at = (rev ? 15 - l16 : l16) * out_pitch + out_col * out_bytes;
+  char* const out_base = (char*)p.out.p + (b * p.out.sb + (h / p.out.group) * p.out.sh) * out_bytes;
+
   // where a lane's operands are in LDS, but for constants: 8 consecutive columns of a row, or one column of 8 rows (of which
   // it supplies 4 columns of one)
-  Lds* const rows_a = (Lds*)As + l16 * X::PA + 8 * g;
-  Lds* const rows_b = (Lds*)Bs + l16 * X::PA + 8 * g;
-  Lds* const rows_p = (Lds*)Ps + l16 * X::PP + 8 * g;
-  Lds* const cols_b = (Lds*)Bs + (8 * g + (l16 >> 2)) * X::PA + 8 * (l16 & 3);
-  Lds* const cols_c = (Lds*)Cs + (8 * g + (l16 >> 2)) * X::PC + 16 * wave + 4 * (l16 & 3);
+  Lds* const rows_a = As + l16 * X::PA + 8 * g;
+  Lds* const rows_b = Bs + l16 * X::PB + 8 * g;
+  Lds* const rows_p = Ps + l16 * X::PP + 8 * g;
+  Lds* const cols_b = Bs + (8 * g + (l16 >> 2)) * X::PB + 8 * (l16 & 3);
+  Lds* const cols_c = Cs + (8 * g + (l16 >> 2)) * X::PC + wave0 + 4 * NB * (l16 & 3);
   auto row_frag = [](Lds* at, int plane) {
     Frag<NS> f;
 #pragma unroll
@@ -348,115 +382,166 @@ const int down = turned ? 4 : dc * 4, lane_at = 8 * g * down + my_col * (turned 
     return f;
   };
 
-  if (p0 < pend) load(p0);
+  if (p0 < pend) {
+    load(p0);
+    store(p0);
+    if (p0 + C < pend) load(p0 + C);
+  }
+  __syncthreads();
   for (int pos = p0; pos < pend; pos += C) {
     const int n = min(C, len - pos);
-    if (!STATE) ra.template store<NS, X::PA>(As, n, rev);
-    rb.template store<NS, X::PA>(Bs, n, rev);
-    rc.template store<NS, X::PC>(Cs, n, rev);
-    if (n < C) update_weights(n);
-    __syncthreads();
-    if (pos + C < pend) load(pos + C);
-
-    f4 out[STATE ? 1 : TB];
+    f4 out[STATE ? 1 : TB][NB];
     if constexpr (!STATE) {
       // scores of the wavefront's blocks, decayed; zero where a position would see one behind it
-      if (tb < TB)
+      // (the places of the block in LDS are worked out for every run: kept, they took registers that are not there, and a
+      // reload from memory waits for the loads of the next run)
+      int tb = wave_tb;
+      asm volatile("" : "+s"(tb));
+      f4 score[BPW];
 #pragma unroll
-        for (int i = 0; i < BPW; ++i) {
-          const int sb = sb0 + i;
-          if (sb > (tb | 1)) continue;
-          f4 acc = {0.f, 0.f, 0.f, 0.f};
-          if (sb <= tb)
-#pragma unroll
-            for (int ks = 0; ks < KS; ++ks)
-              acc = mma(row_frag(rows_b + 16 * sb * X::PA + 32 * ks, C * X::PA), row_frag(rows_a + 16 * tb * X::PA + 32 * ks, C * X::PA), acc);
-          float x[4];
-#pragma unroll
-          for (int r = 0; r < 4; ++r) x[r] = acc[r] * near[i][r];
-          uint32_t w[NS][2];
-          split<NS, 4>(x, w);
-#pragma unroll
-          for (int s = 0; s < NS; ++s) *(u2*)(Ps + s * C * X::PP + (16 * tb + l16) * X::PP + 16 * sb + 4 * g) = (u2){w[s][0], w[s][1]};
-          __builtin_amdgcn_sched_barrier(0);
-        }
-      // what the state before the run gives
-#pragma unroll
-      for (int i = 0; i < TB; ++i) out[i] = (f4){0.f, 0.f, 0.f, 0.f};
+      for (int i = 0; i < BPW; ++i) score[i] = (f4){0.f, 0.f, 0.f, 0.f};
 #pragma unroll
       for (int ks = 0; ks < KS; ++ks) {
-        const f4 lo = S[ks][0], hi = S[ks][1];
-        const float x[8] = {lo[0], lo[1], lo[2], lo[3], hi[0], hi[1], hi[2], hi[3]};
-        const Frag<NS> sf = frag_of<NS>(x);
+        const Frag<NS> q = row_frag(rows_a + 16 * tb * X::PA + 32 * ks, C * X::PA);
 #pragma unroll
-        for (int i = 0; i < TB; ++i) out[i] = mma(sf, row_frag(rows_a + 16 * i * X::PA + 32 * ks, C * X::PA), out[i]);
-        __builtin_amdgcn_sched_barrier(0);  // (moved up, the reads of all steps would take more registers than there are)
+        for (int i = 0; i < BPW; ++i) score[i] = mma(row_frag(rows_b + 16 * (sb0 + i) * X::PB + 32 * ks, C * X::PB), q, score[i]);
       }
+#pragma unroll
+      for (int i = 0; i < BPW; ++i) {
+        const int sb = sb0 + i;
+        float x[4];
+#pragma unroll
+        for (int r = 0; r < 4; ++r) x[r] = score[i][r] * nw[max(16 * (tb - sb) + l16 - 4 * g - r, -1)];
+        uint32_t w[NS][2];
+        split<NS, 4>(x, w);
+#pragma unroll
+        for (int s = 0; s < NS; ++s) *(LdsU2*)(Ps + s * C * X::PP + (16 * tb + l16) * X::PP + 16 * sb + 4 * g) = (u2){w[s][0], w[s][1]};
+      }
+      __builtin_amdgcn_sched_barrier(0);  // (reads of LDS moved further up would take registers that are not there)
+      // what the state before the run gives
 #pragma unroll
       for (int i = 0; i < TB; ++i)
 #pragma unroll
-        for (int r = 0; r < 4; ++r) out[i][r] *= far[i];
+        for (int nb = 0; nb < NB; ++nb) out[i][nb] = (f4){0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+      for (int ks = 0; ks < KS; ++ks) {
+        Frag<NS> sf[NB];
+#pragma unroll
+        for (int nb = 0; nb < NB; ++nb) {
+          const f4 lo = S[ks][0][nb], hi = S[ks][1][nb];
+          const float x[8] = {lo[0], lo[1], lo[2], lo[3], hi[0], hi[1], hi[2], hi[3]};
+          sf[nb] = frag_of<NS>(x);
+        }
+#pragma unroll
+        for (int i = 0; i < TB; ++i) {
+          const Frag<NS> q = row_frag(rows_a + 16 * i * X::PA + 32 * ks, C * X::PA);
+#pragma unroll
+          for (int nb = 0; nb < NB; ++nb) out[i][nb] = mma(sf[nb], q, out[i][nb]);
+        }
+      }
+#pragma unroll
+      for (int i = 0; i < TB; ++i) {
+        const float far = fw[16 * i + l16];
+#pragma unroll
+        for (int nb = 0; nb < NB; ++nb)
+#pragma unroll
+          for (int r = 0; r < 4; ++r) out[i][nb][r] *= far;
+      }
     }
 
+    __builtin_amdgcn_sched_barrier(0);
     // the state after the run
-    const Decay d{pw[n], pl[n]};
+    const double want = run_decay - run_decay * off;
+    const float d = n == C ? (float)want : pw[n];
+    off = ((double)(float)want - want) * per;
 #pragma unroll
     for (int ks = 0; ks < KS; ++ks)
 #pragma unroll
       for (int x = 0; x < 2; ++x)
 #pragma unroll
-        for (int r = 0; r < 4; ++r) S[ks][x][r] = d * S[ks][x][r];
+        for (int nb = 0; nb < NB; ++nb)
+#pragma unroll
+          for (int r = 0; r < 4; ++r) S[ks][x][nb][r] = d * S[ks][x][nb][r];
 #pragma unroll
     for (int ks2 = 0; ks2 < CS; ++ks2) {
-      const f4 w0 = *(const f4*)(uw + 32 * ks2 + 8 * g), w1 = *(const f4*)(uw + 32 * ks2 + 8 * g + 4);
-      float x[8];
-      floats_of<NS>(col_frag(cols_c + 32 * ks2 * X::PC, X::PC), x);
+      Frag<3> wc[NB];
+      const f4 w0 = *(LdsF4*)(uw + 32 * ks2 + 8 * g), w1 = *(LdsF4*)(uw + 32 * ks2 + 8 * g + 4);
 #pragma unroll
-      for (int e = 0; e < 8; ++e) x[e] *= e < 4 ? w0[e & 3] : w1[e & 3];
-      const Frag<3> wc = frag_of<3>(x);
+      for (int nb = 0; nb < NB; ++nb) {
+        float x[8];
+        floats_of<NS>(col_frag(cols_c + 32 * ks2 * X::PC + 4 * nb, X::PC), x);
 #pragma unroll
-      for (int ks = 0; ks < KS; ++ks) {
-#pragma unroll
-        for (int y = 0; y < 2; ++y)
-          S[ks][y] = mma(col_frag(cols_b + 32 * ks2 * X::PA + 32 * ks + 4 * y, X::PA), wc, S[ks][y]);
-        __builtin_amdgcn_sched_barrier(0);
+        for (int e = 0; e < 8; ++e) x[e] *= e < 4 ? w0[e & 3] : w1[e & 3];
+        wc[nb] = frag_of<3>(x);
       }
+#pragma unroll
+      for (int ks = 0; ks < KS; ++ks)
+#pragma unroll
+        for (int y = 0; y < 2; ++y) {
+          const Frag<NS> kt = col_frag(cols_b + 32 * ks2 * X::PB + 32 * ks + 4 * y, X::PB);
+#pragma unroll
+          for (int nb = 0; nb < NB; ++nb) S[ks][y][nb] = mma(kt, wc[nb], S[ks][y][nb]);
+        }
+      __builtin_amdgcn_sched_barrier(0);
     }
+    Frag<NS> cf[CS][NB];
+    if constexpr (!STATE)
+#pragma unroll
+      for (int ks2 = 0; ks2 < CS; ++ks2)
+#pragma unroll
+        for (int nb = 0; nb < NB; ++nb) cf[ks2][nb] = col_frag(cols_c + 32 * ks2 * X::PC + 4 * nb, X::PC);
     __syncthreads();
 
+    // the next run's operands take the place of this one's, of which only the scores are still asked for
+    if (pos + C < pend) {
+      store(pos + C);
+      if (pos + 2 * C < pend) load(pos + 2 * C);
+    }
     if constexpr (!STATE) {
       // what the run's own positions give
 #pragma unroll
-      for (int ks2 = 0; ks2 < CS; ++ks2) {
-        const Frag<NS> cf = col_frag(cols_c + 32 * ks2 * X::PC, X::PC);
+      for (int ks2 = 0; ks2 < CS; ++ks2)
 #pragma unroll
-        for (int i = 2 * ks2; i < TB; ++i) out[i] = mma(cf, row_frag(rows_p + 16 * i * X::PP + 32 * ks2, C * X::PP), out[i]);
-      }
-      // a lane has 4 consecutive columns of one position of each block
-      const int col = tile0 + 16 * wave + 4 * g;
-      const int64_t first = b * p.out.sb + (h / p.out.group) * p.out.sh + col;
+        for (int i = 2 * ks2; i < TB; ++i) {
+          const Frag<NS> pf = row_frag(rows_p + 16 * i * X::PP + 32 * ks2, C * X::PP);
+#pragma unroll
+          for (int nb = 0; nb < NB; ++nb) out[i][nb] = mma(cf[ks2][nb], pf, out[i][nb]);
+        }
+      const __amdgpu_buffer_rsrc_t to = rsrc_of(out_base + (int64_t)(rev ? len - pos - C : pos) * out_pitch);
+      const bool whole = p.out.vec && out_col < dc;
 #pragma unroll
       for (int i = 0; i < TB; ++i) {
-        const int at_i = 16 * i + l16;
-        if (at_i >= n) continue;
-        const int64_t to = first + (int64_t)(rev ? len - 1 - pos - at_i : pos + at_i) * p.out.st;
+        const int step = (rev ? TB - 1 - i : i) * 16 * out_pitch;
+        const bool there = 16 * i + l16 < n;
         if (p.out_f32 || sizeof(T) == 4) {
-          float* o = (float*)p.out.p + to;
-          if (p.out.vec && col < dc)
-            *(f4*)o = out[i];
-          else
 #pragma unroll
-            for (int e = 0; e < 4; ++e)
-              if (col + e < dc) o[e] = out[i][e];
+          for (int nb = 0; nb < NB; ++nb)
+            if (p.out.vec)
+              __builtin_amdgcn_raw_buffer_store_b128(__builtin_bit_cast(u4, out[i][nb]), to,
+                                                     there && out_col + 4 * nb < dc ? out_at + 16 * nb : kPast, step, 0);
+            else
+#pragma unroll
+              for (int e = 0; e < 4; ++e)
+                __builtin_amdgcn_raw_buffer_store_b32(__float_as_uint(out[i][nb][e]), to,
+                                                      there && out_col + 4 * nb + e < dc ? out_at + 16 * nb + 4 * e : kPast, step, 0);
         } else {
-          uint16_t* o = (uint16_t*)p.out.p + to;
-          const u2 w = {pack_bf16(out[i][0], out[i][1]), pack_bf16(out[i][2], out[i][3])};
-          if (p.out.vec && col < dc)
-            *(u2*)o = w;
-          else
+          uint32_t w[2 * NB];
 #pragma unroll
-            for (int e = 0; e < 4; ++e)
-              if (col + e < dc) o[e] = (uint16_t)(w[e / 2] >> (16 * (e & 1)));
+          for (int nb = 0; nb < NB; ++nb) {
+            w[2 * nb] = pack_bf16(out[i][nb][0], out[i][nb][1]);
+            w[2 * nb + 1] = pack_bf16(out[i][nb][2], out[i][nb][3]);
+          }
+          if (p.out.vec) {  // (rows are multiples of 8 then)
+            if constexpr (NB == 2)
+              __builtin_amdgcn_raw_buffer_store_b128((u4){w[0], w[1], w[2], w[3]}, to, there && whole ? out_at : kPast, step, 0);
+            else
+              __builtin_amdgcn_raw_buffer_store_b64((u2){w[0], w[1]}, to, there && whole ? out_at : kPast, step, 0);
+          } else {
+#pragma unroll
+            for (int e = 0; e < 4 * NB; ++e)
+              __builtin_amdgcn_raw_buffer_store_b16((uint16_t)(w[e / 2] >> (16 * (e & 1))), to,
+                                                    there && out_col + e < dc ? out_at + 2 * e : kPast, step, 0);
+          }
         }
       }
     }
@@ -478,18 +563,21 @@ const int down = turned ? 4 : dc * 4, lane_at = 8 * g * down + my_col * (turned 
   // the state: of the segment for the prefix sum (it enters the next one), or behind all of them
   float* const into = STATE ? sg.states + seg_at + elems : (p.s_out && slot >= 0 && seg == sg.n - 1 ? p.s_out + at : nullptr);
   if (into) {
-    const int lane_at = 8 * g * dc * 4 + my_col * 4;
-    int rows = da - 8 * g;
+    int rows = da - 4 * g;
     asm volatile("" : "+v"(rows));  // (the conditions of the first loads of S are not to be kept until here)
 #pragma unroll
     for (int ks = 0; ks < KS; ++ks)
 #pragma unroll
       for (int x = 0; x < 2; ++x)
 #pragma unroll
-        for (int r = 0; r < 4; ++r) {
-          const int row = 32 * ks + 4 * x + r;
-          __builtin_amdgcn_raw_buffer_store_b32(__float_as_uint(S[ks][x][r]), rsrc_of(into),
-                                                my_col < dc && row < rows ? lane_at : kPast, row * dc * 4, 0);
+        for (int nb = 0; nb < NB; ++nb) {
+          const int col = col_of(l16, nb), lane_at = 4 * g * dc * 4 + col * 4;
+#pragma unroll
+          for (int r = 0; r < 4; ++r) {
+            const int row = 32 * ks + 16 * x + r;
+            __builtin_amdgcn_raw_buffer_store_b32(__float_as_uint(S[ks][x][nb][r]), rsrc_of(into),
+                                                  col < dc && row < rows ? lane_at : kPast, row * dc * 4, 0);
+          }
         }
   }
 }
@@ -540,40 +628,37 @@ __global__ __launch_bounds__(256) void linattn_share_kernel(const float* __restr
   ((T*)dst.p)[bt / T_ * dst.sb + bt % T_ * dst.st + hs * dst.sh + ch] = from_float<T>(sum);
 }
 
-template <typename T, int KP, int W, bool STATE>
+template <typename T, int KP, int NB, bool STATE>
 mdh_status run(const PassArgs& a, hipStream_t st) {
-  using X = Shape<T, KP, W, STATE>;
+  using X = Shape<T, KP, NB, STATE>;
   static int64_t done[kMaxDevices];
   int tiles = 0;
   for (int i = 0; i < a.n; ++i) tiles += a.tiles[i];
   const int64_t blocks = a.c.B * a.c.H * (STATE ? a.seg[0].n - 1 : a.seg[0].n) * tiles;
   if (blocks > 0x7fffffff) return MDH_ERR_SIZE;
-  const void* kern = (const void*)linattn_runs_kernel<T, KP, W, STATE>;
+  const void* kern = (const void*)linattn_runs_kernel<T, KP, NB, STATE>;
   const mdh_status r = allow_dynamic_lds(kern, X::kBytes, done);
   if (r != MDH_OK) return r;
   clear_stale_error();
-  linattn_runs_kernel<T, KP, W, STATE><<<dim3((unsigned)blocks), 64 * W, X::kBytes, st>>>(a);
+  linattn_runs_kernel<T, KP, NB, STATE><<<dim3((unsigned)blocks), kThreads, X::kBytes, st>>>(a);
   return launch_status();
 }
 
-template <typename T, int KP, bool STATE>
-mdh_status run(const PassArgs& a, int W, hipStream_t st) {
-  return W == 8 ? run<T, KP, 8, STATE>(a, st) : run<T, KP, 4, STATE>(a, st);
-}
-
 template <typename T, bool STATE>
-mdh_status run(const PassArgs& a, int KP, int W, hipStream_t st) {
-  return KP == 64 ? run<T, 64, STATE>(a, W, st) : KP == 128 ? run<T, 128, STATE>(a, W, st) : run<T, 256, STATE>(a, W, st);
+mdh_status run(const PassArgs& a, int KP, int NB, hipStream_t st) {
+  if (KP == 256) return run<T, 256, 1, STATE>(a, st);
+  if (KP == 128) return NB == 2 ? run<T, 128, 2, STATE>(a, st) : run<T, 128, 1, STATE>(a, st);
+  return NB == 2 ? run<T, 64, 2, STATE>(a, st) : run<T, 64, 1, STATE>(a, st);
 }
 
 template <bool STATE>
-mdh_status run(const PassArgs& a, int dtype, int KP, int W, hipStream_t st) {
-  return dtype == MDH_BF16 ? run<bf16, STATE>(a, KP, W, st) : run<float, STATE>(a, KP, W, st);
+mdh_status run(const PassArgs& a, int dtype, int KP, int NB, hipStream_t st) {
+  return dtype == MDH_BF16 ? run<bf16, STATE>(a, KP, NB, st) : run<float, STATE>(a, KP, NB, st);
 }
 
 int padded(int da) { return da <= 64 ? 64 : da <= 128 ? 128 : 256; }
-// wavefronts: of 16 columns each
-int waves_of(int dc) { return dc > 64 ? 8 : 4; }
+// column blocks of a wavefront: two where there are columns for them and the registers hold the state
+int blocks_of(int KP, int dc) { return KP <= 128 && dc > 64 ? 2 : 1; }
 
 // Segments of T positions, of whole runs: enough that `work` workgroups for each fill the chip twice.
 int segments_of(int64_t T, int C, int64_t work, int64_t* len) {
@@ -585,7 +670,7 @@ int segments_of(int64_t T, int C, int64_t work, int64_t* len) {
   return T > 0 ? (int)cdiv(T, *len) : 1;
 }
 int run_length(int dtype) { return dtype == MDH_BF16 ? 64 : 32; }
-int64_t tiles_of(int dc) { return cdiv(dc, 16 * waves_of(dc)); }
+int64_t tiles_of(int da, int dc) { return cdiv(dc, 64 * blocks_of(padded(da), dc)); }
 
 }  // namespace
 
@@ -597,7 +682,7 @@ size_t linattn_segment_bytes(int64_t B, int64_t T, int H, int dk, int dv, int dt
 }
 
 int linattn_segments(int64_t B, int64_t T, int H, int dk, int dv, int dtype, bool backward, int64_t* len) {
-  const int64_t work = B * H * (backward ? tiles_of(dk) * 2 + tiles_of(dv) : tiles_of(dv));
+  const int64_t work = B * H * (backward ? tiles_of(dv, dk) * 2 + tiles_of(dk, dv) : tiles_of(dk, dv));
   return segments_of(T, run_length(dtype), work, len);
 }
 
@@ -607,13 +692,13 @@ mdh_status launch_linattn_segments(const LinattnCall& c, const LinattnPass* p, i
   PassArgs a{};
   a.c = c;
   a.n = np;
-  const int KP = padded(p[0].da), W = waves_of(p[0].dc);
+  const int KP = padded(p[0].da), NB = blocks_of(KP, p[0].dc);
   for (int i = 0; i < np; ++i) {
     a.p[i] = p[i];
-    a.tiles[i] = (int)cdiv(p[i].dc, 16 * W);
+    a.tiles[i] = (int)cdiv(p[i].dc, 64 * NB);
     a.seg[i] = SegmentArgs{n, len, states[i]};
   }
-  mdh_status r = run<true>(a, dtype, KP, W, st);
+  mdh_status r = run<true>(a, dtype, KP, NB, st);
   for (int i = 0; i < np && r == MDH_OK; ++i) {
     const CombineArgs k{c, a.seg[i], p[i].s_in, (int64_t)p[i].da * p[i].dc};
     clear_stale_error();
@@ -629,19 +714,19 @@ mdh_status launch_linattn_pass(const LinattnCall& c, const LinattnPass* passes, 
   bool gone[3] = {};
   for (int i = 0; i < np; ++i) {
     if (gone[i]) continue;
-    const int KP = padded(passes[i].da), W = waves_of(passes[i].dc);
+    const int KP = padded(passes[i].da), NB = blocks_of(KP, passes[i].dc);
     PassArgs a{};
     a.c = c;
     for (int j = i; j < np; ++j) {
-      if (gone[j] || padded(passes[j].da) != KP || waves_of(passes[j].dc) != W) continue;
+      if (gone[j] || padded(passes[j].da) != KP || blocks_of(KP, passes[j].dc) != NB) continue;
       gone[j] = true;
       a.p[a.n] = passes[j];
-      a.tiles[a.n] = (int)cdiv(passes[j].dc, 16 * W);
+      a.tiles[a.n] = (int)cdiv(passes[j].dc, 64 * NB);
       a.seg[a.n] = SegmentArgs{n, len, states[j]};
       a.seg_t[a.n] = turned[j];
       ++a.n;
     }
-    const mdh_status r = run<false>(a, dtype, KP, W, st);
+    const mdh_status r = run<false>(a, dtype, KP, NB, st);
     if (r != MDH_OK) return r;
   }
   return MDH_OK;
