@@ -108,76 +108,88 @@ __device__ __forceinline__ f4 mma(const Frag<NA>& a, const Frag<NB>& b, f4 acc) 
   return acc;
 }
 
-// 8 consecutive channels of a row as they come from memory, at byte `at` + `step` of a descriptor whose loads past its 2^31
-// bytes give 0: parts that are not there are asked for past the end.  VEC: 16 bytes at a time, else element by element
-// (any alignment).
 constexpr int kWaves = 4, kThreads = 64 * kWaves;
+
+// How rows are read and written (one kernel for each: what the general ones keep in registers would cost the first its speed).
+//   kVec   16 bytes at a time: bases, strides and rows are multiples of 16 bytes
+//   kAny   16 bytes at a time at any address; the row's last ones are read as the 16 bytes that end with it and moved down
+//          (rows have 16 bytes at least)
+//   kEach  element by element: shorter rows
+enum Access { kVec = 0, kAny = 1, kEach = 2 };
+
+// Loads go through a descriptor whose loads past its 2^31 bytes give 0: what is not there is asked for past the end.
 constexpr int kPast = (int)0x80000000;
 __device__ __forceinline__ __amdgpu_buffer_rsrc_t rsrc_of(const void* p) {
   return __builtin_amdgcn_make_buffer_rsrc(const_cast<void*>(p), 0, 0x7fffffff, 0x00027000);
 }
-// LOADS of them for 8 channels; each has its own place, past the end where its channels are not there.
-template <typename T>
-struct Raw {
-  static constexpr int kLoads = sizeof(T) / 2, kPer = 16 / sizeof(T);  // 16-byte loads of a piece, channels of one
-  u4 w[kLoads];
-  __device__ __forceinline__ void load(__amdgpu_buffer_rsrc_t from, const int (&at)[kLoads], int step) {
-#pragma unroll
-    for (int i = 0; i < kLoads; ++i) w[i] = __builtin_amdgcn_raw_buffer_load_b128(from, at[i], step, 0);
-  }
-  __device__ __forceinline__ void load_each(__amdgpu_buffer_rsrc_t from, int at, int step, int d) {
-    if constexpr (sizeof(T) == 2) {
-#pragma unroll
-      for (int e = 0; e < 4; ++e) {
-        const uint32_t lo = __builtin_amdgcn_raw_buffer_load_b16(from, 2 * e < d ? at + 4 * e : kPast, step, 0);
-        const uint32_t hi = __builtin_amdgcn_raw_buffer_load_b16(from, 2 * e + 1 < d ? at + 4 * e + 2 : kPast, step, 0);
-        w[0][e] = (lo & 0xffffu) | hi << 16;
-      }
-    } else {
-#pragma unroll
-      for (int e = 0; e < 8; ++e) w[e / 4][e & 3] = __builtin_amdgcn_raw_buffer_load_b32(from, e < d ? at + 4 * e : kPast, step, 0);
-    }
-  }
-};
 
 // The rows of one operand that a run reads: the lane has channels col.. of positions row, row + kStep, .. of it
-template <typename T, int C, int WIDE>
+template <typename T, int C, int WIDE, int ACCESS>
 struct Rows {
   static constexpr int kAcross = WIDE / 8, kStep = kThreads / kAcross, N = C / kStep;
+  static constexpr int kLoads = sizeof(T) / 2, kPer = 16 / sizeof(T);  // 16-byte loads of 8 channels, channels of one
   static_assert(C % kStep == 0 && N >= 1, "every lane has whole rows");
-  Raw<T> r[N];
-  int at[Raw<T>::kLoads], pitch, rev;
+  u4 w[N][kLoads];
+  int at[kLoads], pitch, rev;
+  int down[ACCESS == kAny ? kLoads : 1];  // channels that a load's are moved down by
   const T* base;  // position 0's row would be here, were all runs full
   int64_t st;
   static __device__ __forceinline__ int col() { return threadIdx.x % kAcross * 8; }
   static __device__ __forceinline__ int row() { return threadIdx.x / kAcross; }
-  __device__ __forceinline__ void init(const HeadView& v, int64_t offset, int d, int rev_) {
+  __device__ __forceinline__ void init(const HeadView& v, int64_t offset, int col0, int d, int rev_) {  // channels from col0 on, of rows of d
     base = (const T*)v.p + offset;
     st = v.st;
     pitch = (int)(v.st * sizeof(T));
     rev = rev_;
-    const int first = (rev ? C - 1 - row() - (N - 1) * kStep : row()) * pitch + col() * (int)sizeof(T);
+    const int first = (rev ? C - 1 - row() - (N - 1) * kStep : row()) * pitch;
 #pragma unroll
-    for (int i = 0; i < Raw<T>::kLoads; ++i) at[i] = col() + i * Raw<T>::kPer < d ? first + 16 * i : kPast;
+    for (int i = 0; i < kLoads; ++i) {
+      const int c = col0 + col() + i * kPer;
+      at[i] = ACCESS == kEach || c < d ? first + c * (int)sizeof(T) : kPast;
+      if (ACCESS == kAny) {
+        down[i] = c < d && c + kPer > d ? c + kPer - d : 0;
+        at[i] -= down[i] * (int)sizeof(T);
+      }
+    }
   }
-  // the run of n positions whose first is pos, of len (all loads of a sequence's last run, which may be shorter, are checked)
-  __device__ __forceinline__ void load(int vec, int pos, int n, int len, int d) {
+  // the run of n positions whose first is pos, of len (the loads of a sequence's last run, which may be shorter, are checked)
+  __device__ __forceinline__ void load(int pos, int n, int len, int d) {
     const __amdgpu_buffer_rsrc_t from = rsrc_of(base + (int64_t)(rev ? len - pos - C : pos) * st);
 #pragma unroll
     for (int j = 0; j < N; ++j) {
       const int step = (rev ? N - 1 - j : j) * kStep * pitch;
-      if (vec && n == C) {
-        r[j].load(from, at, step);
-      } else if (vec) {
-        int checked[Raw<T>::kLoads];
+      const bool there = row() + j * kStep < n;
 #pragma unroll
-        for (int i = 0; i < Raw<T>::kLoads; ++i) checked[i] = row() + j * kStep < n ? at[i] : kPast;
-        r[j].load(from, checked, step);
-      } else {
-        const int first = (rev ? C - 1 - row() - (N - 1) * kStep : row()) * pitch + col() * (int)sizeof(T);
-        r[j].load_each(from, first, step, row() + j * kStep < n ? d - col() : 0);
+      for (int i = 0; i < kLoads; ++i) {
+        if constexpr (ACCESS == kEach) {
+          const int left = there ? d - col() - i * kPer : 0;
+#pragma unroll
+          for (int e = 0; e < 4; ++e)
+            if constexpr (sizeof(T) == 4) {
+              w[j][i][e] = __builtin_amdgcn_raw_buffer_load_b32(from, e < left ? at[i] + 4 * e : kPast, step, 0);
+            } else {
+              const uint32_t lo = __builtin_amdgcn_raw_buffer_load_b16(from, 2 * e < left ? at[i] + 4 * e : kPast, step, 0);
+              const uint32_t hi = __builtin_amdgcn_raw_buffer_load_b16(from, 2 * e + 1 < left ? at[i] + 4 * e + 2 : kPast, step, 0);
+              w[j][i][e] = (lo & 0xffffu) | hi << 16;
+            }
+        } else if (n == C) {
+          w[j][i] = __builtin_amdgcn_raw_buffer_load_b128(from, at[i], step, 0);
+        } else {
+          w[j][i] = __builtin_amdgcn_raw_buffer_load_b128(from, there ? at[i] : kPast, step, 0);
+        }
       }
     }
+  }
+  // what load j has left of its channels, moved down to where they belong
+  __device__ __forceinline__ u4 placed(int j, int i) const {
+    u4 v = w[j][i];
+    if constexpr (ACCESS == kAny) {
+      const int words = sizeof(T) == 4 ? down[i] : down[i] >> 1;
+      if (words & 2) v = (u4){v[2], v[3], 0, 0};
+      if (words & 1) v = (u4){v[1], v[2], v[3], 0};
+      if (sizeof(T) == 2 && (down[i] & 1)) v = (u4){v[0] >> 16 | v[1] << 16, v[1] >> 16 | v[2] << 16, v[2] >> 16 | v[3] << 16, v[3] >> 16};
+    }
+    return v;
   }
   // PAIRED: of 32 channels, 4g.. and 16 + 4g.. side by side
   template <int NS, int PITCH, bool PAIRED = false>
@@ -188,11 +200,12 @@ struct Rows {
     for (int j = 0; j < N; ++j) {
       Frag<NS> f;
       if constexpr (NS == 1) {
-        f.s[0] = r[j].w[0];
+        f.s[0] = placed(j, 0);
       } else {
+        const u4 lo = placed(j, 0), hi = placed(j, kLoads - 1);
         float x[8];
 #pragma unroll
-        for (int e = 0; e < 8; ++e) x[e] = __uint_as_float(r[j].w[e / 4][e & 3]);
+        for (int e = 0; e < 8; ++e) x[e] = __uint_as_float(e < 4 ? lo[e & 3] : hi[e & 3]);
         f = frag_of<NS>(x);
       }
 #pragma unroll
@@ -210,7 +223,8 @@ struct Rows {
 };
 
 // The shape of a kernel: KP rows of the state (da padded), four wavefronts with NB blocks of 16 columns each.  Two blocks where
-// they can be: what a wavefront reads of a, b and the scores serves both, and LDS is what the passes are short of.
+// they can be: what a wavefront reads of a, b and the scores serves both, and LDS is what the passes are short of (32 x 4096
+// x 16 x 128 x 128, forward: 495 us; one block each for eight wavefronts 579).
 template <typename T, int KP_, int NB_, bool STATE_>
 struct Shape {
   static constexpr int NS = sizeof(T) == 2 ? 1 : 3;
@@ -242,10 +256,10 @@ struct PassArgs {
   int seg_t[3];     // the states are (dc, da) of this pass
 };
 
-template <typename T, int KP, int NB, bool STATE>
-__global__ __launch_bounds__(kThreads, 2) void linattn_runs_kernel(PassArgs args) {
+template <typename T, int KP, int NB, bool STATE, int ACCESS>
+__global__ __launch_bounds__(kThreads, ACCESS == kEach ? 2 : KP == 64 && NB == 1 ? 4 : KP == 128 && NB == 1 ? 3 : 2) void linattn_runs_kernel(PassArgs args) {
   using X = Shape<T, KP, NB, STATE>;
-  constexpr int C = X::C, NS = X::NS, TB = X::TB, KS = X::KS, CS = X::CS, TH = kThreads;
+  constexpr int C = X::C, NS = X::NS, TB = X::TB, KS = X::KS, CS = X::CS;
   extern __shared__ __align__(16) uint16_t lds[];
   Lds* const As = (Lds*)lds + X::A;
   Lds* const Bs = (Lds*)lds + X::B;
@@ -336,22 +350,24 @@ __global__ __launch_bounds__(kThreads, 2) void linattn_runs_kernel(PassArgs args
   const int wave_tb = wave * BPW / TB, sb0 = wave * BPW % TB;
 
   // operands: the rows of the next run, in registers until this one is done
-  Rows<T, C, KP> ra, rb;
-  Rows<T, C, X::VT> rc;
-  if (!STATE) ra.init(p.a, b * p.a.sb + (h / p.a.group) * p.a.sh, da, rev);
-  rb.init(p.b, b * p.b.sb + (h / p.b.group) * p.b.sh, da, rev);
-  rc.init(p.c, b * p.c.sb + (h / p.c.group) * p.c.sh + tile0, dc - tile0, rev);
+  Rows<T, C, KP, ACCESS> ra, rb;
+  Rows<T, C, X::VT, ACCESS> rc;
+  if (!STATE) ra.init(p.a, b * p.a.sb + (h / p.a.group) * p.a.sh, 0, da, rev);
+  rb.init(p.b, b * p.b.sb + (h / p.b.group) * p.b.sh, 0, da, rev);
+  rc.init(p.c, b * p.c.sb + (h / p.c.group) * p.c.sh, tile0, dc, rev);
   auto load = [&](int pos) {
+    if (pos < p0 || pos >= pend) return;
     const int n = min(C, len - pos);
-    if (!STATE) ra.load(p.a.vec, pos, n, len, da);
-    rb.load(p.b.vec, pos, n, len, da);
-    rc.load(p.c.vec, pos, n, len, dc - tile0);
+    if (!STATE) ra.load(pos, n, len, da);
+    rb.load(pos, n, len, da);
+    rc.load(pos, n, len, dc - tile0);
   };
   auto store = [&](int pos) {
+    if (pos < p0 || pos >= pend) return;
     if (!STATE) ra.template store<NS, X::PA, true>(As);
     rb.template store<NS, X::PB, true>(Bs);
     rc.template store<NS, X::PC>(Cs);
-    if (len - pos < C) update_weights(len - pos);
+    if (!STATE && len - pos < C) update_weights(len - pos);
   };
   // outputs: a lane has 4 NB consecutive columns of position l16 of each block of 16
   const int out_bytes = p.out_f32 ? 4 : (int)sizeof(T), out_pitch = (int)(p.out.st * out_bytes);
@@ -382,13 +398,16 @@ __global__ __launch_bounds__(kThreads, 2) void linattn_runs_kernel(PassArgs args
     return f;
   };
 
-  if (p0 < pend) {
-    load(p0);
-    store(p0);
-    if (p0 + C < pend) load(p0 + C);
-  }
+  // A sum of states is made from the last run to the first, each times the decay of those behind it: the runs that are read
+  // first by the pass afterwards are the ones that the chip's cache has seen last.
+  const int runs = (pend - p0 + C - 1) / C, first = STATE ? p0 + (runs - 1) * C : p0, next = STATE ? -C : C;
+  double behind = 1.0;  // STATE: the decay of the runs behind this one
+  load(first);
+  store(first);
+  load(first + next);
+  if (STATE && runs > 0 && pend - first < C) update_weights(pend - first);
   __syncthreads();
-  for (int pos = p0; pos < pend; pos += C) {
+  for (int i_run = 0, pos = first; i_run < runs; ++i_run, pos += next) {
     const int n = min(C, len - pos);
     f4 out[STATE ? 1 : TB][NB];
     if constexpr (!STATE) {
@@ -451,21 +470,30 @@ __global__ __launch_bounds__(kThreads, 2) void linattn_runs_kernel(PassArgs args
 
     __builtin_amdgcn_sched_barrier(0);
     // the state after the run
-    const double want = run_decay - run_decay * off;
-    const float d = n == C ? (float)want : pw[n];
-    off = ((double)(float)want - want) * per;
+    const float times = (float)behind;
+    if constexpr (STATE) {
+      if (times == 0.f) break;  // (for everybody alike; nothing further back is left of)
+      behind *= n == C ? run_decay : (double)pw[n];
+    } else {
+      const double want = run_decay - run_decay * off;
+      const float d = n == C ? (float)want : pw[n];
+      off = ((double)(float)want - want) * per;
 #pragma unroll
-    for (int ks = 0; ks < KS; ++ks)
+      for (int ks = 0; ks < KS; ++ks)
 #pragma unroll
-      for (int x = 0; x < 2; ++x)
+        for (int x = 0; x < 2; ++x)
 #pragma unroll
-        for (int nb = 0; nb < NB; ++nb)
+          for (int nb = 0; nb < NB; ++nb)
 #pragma unroll
-          for (int r = 0; r < 4; ++r) S[ks][x][nb][r] = d * S[ks][x][nb][r];
+            for (int r = 0; r < 4; ++r) S[ks][x][nb][r] = d * S[ks][x][nb][r];
+    }
 #pragma unroll
     for (int ks2 = 0; ks2 < CS; ++ks2) {
       Frag<3> wc[NB];
-      const f4 w0 = *(LdsF4*)(uw + 32 * ks2 + 8 * g), w1 = *(LdsF4*)(uw + 32 * ks2 + 8 * g + 4);
+      f4 w0 = *(LdsF4*)(uw + 32 * ks2 + 8 * g), w1 = *(LdsF4*)(uw + 32 * ks2 + 8 * g + 4);
+      if (STATE)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) w0[e] *= times, w1[e] *= times;
 #pragma unroll
       for (int nb = 0; nb < NB; ++nb) {
         float x[8];
@@ -482,7 +510,7 @@ __global__ __launch_bounds__(kThreads, 2) void linattn_runs_kernel(PassArgs args
 #pragma unroll
           for (int nb = 0; nb < NB; ++nb) S[ks][y][nb] = mma(kt, wc[nb], S[ks][y][nb]);
         }
-      __builtin_amdgcn_sched_barrier(0);
+      if (!STATE) __builtin_amdgcn_sched_barrier(0);
     }
     Frag<NS> cf[CS][NB];
     if constexpr (!STATE)
@@ -493,10 +521,9 @@ __global__ __launch_bounds__(kThreads, 2) void linattn_runs_kernel(PassArgs args
     __syncthreads();
 
     // the next run's operands take the place of this one's, of which only the scores are still asked for
-    if (pos + C < pend) {
-      store(pos + C);
-      if (pos + 2 * C < pend) load(pos + 2 * C);
-    }
+    store(pos + next);
+    if (STATE && n < C) update_weights(C);
+    load(pos + 2 * next);
     if constexpr (!STATE) {
       // what the run's own positions give
 #pragma unroll
@@ -508,22 +535,22 @@ __global__ __launch_bounds__(kThreads, 2) void linattn_runs_kernel(PassArgs args
           for (int nb = 0; nb < NB; ++nb) out[i][nb] = mma(cf[ks2][nb], pf, out[i][nb]);
         }
       const __amdgpu_buffer_rsrc_t to = rsrc_of(out_base + (int64_t)(rev ? len - pos - C : pos) * out_pitch);
-      const bool whole = p.out.vec && out_col < dc;
 #pragma unroll
       for (int i = 0; i < TB; ++i) {
         const int step = (rev ? TB - 1 - i : i) * 16 * out_pitch;
         const bool there = 16 * i + l16 < n;
         if (p.out_f32 || sizeof(T) == 4) {
 #pragma unroll
-          for (int nb = 0; nb < NB; ++nb)
-            if (p.out.vec)
-              __builtin_amdgcn_raw_buffer_store_b128(__builtin_bit_cast(u4, out[i][nb]), to,
-                                                     there && out_col + 4 * nb < dc ? out_at + 16 * nb : kPast, step, 0);
-            else
+          for (int nb = 0; nb < NB; ++nb) {
+            const int c = out_col + 4 * nb, to_c = out_at + 16 * nb;
+            const bool whole = ACCESS == kVec ? c < dc : c + 4 <= dc;  // (rows of fp32 partial sums: their own multiple of 4)
+            __builtin_amdgcn_raw_buffer_store_b128(__builtin_bit_cast(u4, out[i][nb]), to, there && whole ? to_c : kPast, step, 0);
+            if (ACCESS != kVec)
 #pragma unroll
-              for (int e = 0; e < 4; ++e)
+              for (int e = 0; e < 3; ++e)
                 __builtin_amdgcn_raw_buffer_store_b32(__float_as_uint(out[i][nb][e]), to,
-                                                      there && out_col + 4 * nb + e < dc ? out_at + 16 * nb + 4 * e : kPast, step, 0);
+                                                      there && !whole && c + e < dc ? to_c + 4 * e : kPast, step, 0);
+          }
         } else {
           uint32_t w[2 * NB];
 #pragma unroll
@@ -531,17 +558,16 @@ __global__ __launch_bounds__(kThreads, 2) void linattn_runs_kernel(PassArgs args
             w[2 * nb] = pack_bf16(out[i][nb][0], out[i][nb][1]);
             w[2 * nb + 1] = pack_bf16(out[i][nb][2], out[i][nb][3]);
           }
-          if (p.out.vec) {  // (rows are multiples of 8 then)
-            if constexpr (NB == 2)
-              __builtin_amdgcn_raw_buffer_store_b128((u4){w[0], w[1], w[2], w[3]}, to, there && whole ? out_at : kPast, step, 0);
-            else
-              __builtin_amdgcn_raw_buffer_store_b64((u2){w[0], w[1]}, to, there && whole ? out_at : kPast, step, 0);
-          } else {
+          const bool whole = ACCESS == kVec ? out_col < dc : out_col + 4 * NB <= dc;
+          if constexpr (NB == 2)
+            __builtin_amdgcn_raw_buffer_store_b128((u4){w[0], w[1], w[2], w[3]}, to, there && whole ? out_at : kPast, step, 0);
+          else
+            __builtin_amdgcn_raw_buffer_store_b64((u2){w[0], w[1]}, to, there && whole ? out_at : kPast, step, 0);
+          if (ACCESS != kVec)
 #pragma unroll
-            for (int e = 0; e < 4 * NB; ++e)
+            for (int e = 0; e < 4 * NB - 1; ++e)
               __builtin_amdgcn_raw_buffer_store_b16((uint16_t)(w[e / 2] >> (16 * (e & 1))), to,
-                                                    there && out_col + e < dc ? out_at + 2 * e : kPast, step, 0);
-          }
+                                                    there && !whole && out_col + e < dc ? out_at + 2 * e : kPast, step, 0);
         }
       }
     }
@@ -552,7 +578,7 @@ __global__ __launch_bounds__(kThreads, 2) void linattn_runs_kernel(PassArgs args
     // tokens behind the last valid one
     const int64_t begin = max((int64_t)len, seg * sg.len), end = min(call.T, (seg + 1) * sg.len);
     const int cols = min(dc - tile0, X::VT);
-    for (int64_t i = begin * cols + tid; i < end * cols; i += TH) {
+    for (int64_t i = begin * cols + tid; i < end * cols; i += kThreads) {
       const int64_t to = b * p.out.sb + (h / p.out.group) * p.out.sh + i / cols * p.out.st + tile0 + i % cols;
       if (p.out_f32 || sizeof(T) == 4)
         ((float*)p.out.p)[to] = 0.f;
@@ -628,7 +654,7 @@ __global__ __launch_bounds__(256) void linattn_share_kernel(const float* __restr
   ((T*)dst.p)[bt / T_ * dst.sb + bt % T_ * dst.st + hs * dst.sh + ch] = from_float<T>(sum);
 }
 
-template <typename T, int KP, int NB, bool STATE>
+template <typename T, int KP, int NB, bool STATE, int ACCESS>
 mdh_status run(const PassArgs& a, hipStream_t st) {
   using X = Shape<T, KP, NB, STATE>;
   static int64_t done[kMaxDevices];
@@ -636,41 +662,46 @@ mdh_status run(const PassArgs& a, hipStream_t st) {
   for (int i = 0; i < a.n; ++i) tiles += a.tiles[i];
   const int64_t blocks = a.c.B * a.c.H * (STATE ? a.seg[0].n - 1 : a.seg[0].n) * tiles;
   if (blocks > 0x7fffffff) return MDH_ERR_SIZE;
-  const void* kern = (const void*)linattn_runs_kernel<T, KP, NB, STATE>;
+  const void* kern = (const void*)linattn_runs_kernel<T, KP, NB, STATE, ACCESS>;
   const mdh_status r = allow_dynamic_lds(kern, X::kBytes, done);
   if (r != MDH_OK) return r;
   clear_stale_error();
-  linattn_runs_kernel<T, KP, NB, STATE><<<dim3((unsigned)blocks), kThreads, X::kBytes, st>>>(a);
+  linattn_runs_kernel<T, KP, NB, STATE, ACCESS><<<dim3((unsigned)blocks), kThreads, X::kBytes, st>>>(a);
   return launch_status();
 }
 
+template <typename T, bool STATE, int ACCESS>
+mdh_status run_one(const PassArgs& a, int KP, hipStream_t st) {
+  return KP == 64 ? run<T, 64, 1, STATE, ACCESS>(a, st)
+                  : KP == 128 ? run<T, 128, 1, STATE, ACCESS>(a, st) : run<T, 256, 1, STATE, ACCESS>(a, st);
+}
+
 template <typename T, bool STATE>
-mdh_status run(const PassArgs& a, int KP, int NB, hipStream_t st) {
-  if (KP == 256) return run<T, 256, 1, STATE>(a, st);
-  if (KP == 128) return NB == 2 ? run<T, 128, 2, STATE>(a, st) : run<T, 128, 1, STATE>(a, st);
-  return NB == 2 ? run<T, 64, 2, STATE>(a, st) : run<T, 64, 1, STATE>(a, st);
+mdh_status run(const PassArgs& a, int KP, int NB, int access, hipStream_t st) {
+  if (access == kAny) return run_one<T, STATE, kAny>(a, KP, st);
+  if (access == kEach) return run_one<T, STATE, kEach>(a, KP, st);
+  if (NB == 1) return run_one<T, STATE, kVec>(a, KP, st);
+  return KP == 128 ? run<T, 128, 2, STATE, kVec>(a, st) : run<T, 64, 2, STATE, kVec>(a, st);
 }
 
 template <bool STATE>
-mdh_status run(const PassArgs& a, int dtype, int KP, int NB, hipStream_t st) {
-  return dtype == MDH_BF16 ? run<bf16, STATE>(a, KP, NB, st) : run<float, STATE>(a, KP, NB, st);
+mdh_status run(const PassArgs& a, int dtype, int KP, int NB, int access, hipStream_t st) {
+  return dtype == MDH_BF16 ? run<bf16, STATE>(a, KP, NB, access, st) : run<float, STATE>(a, KP, NB, access, st);
+}
+
+// The kernel for a pass's operands and output.
+int access_of(const LinattnPass& p, int dtype, bool output) {
+  if (p.a.vec && p.b.vec && p.c.vec && (!output || p.out.vec)) return kVec;
+  const int row = dtype == MDH_BF16 ? 8 : 4;
+  return p.da >= row && p.dc >= row ? kAny : kEach;
 }
 
 int padded(int da) { return da <= 64 ? 64 : da <= 128 ? 128 : 256; }
 // column blocks of a wavefront: two where there are columns for them and the registers hold the state
-int blocks_of(int KP, int dc) { return KP <= 128 && dc > 64 ? 2 : 1; }
+int blocks_of(int KP, int dc, int access) { return access == kVec && KP <= 128 && dc > 64 ? 2 : 1; }
 
-// Segments of T positions, of whole runs: enough that `work` workgroups for each fill the chip twice.
-int segments_of(int64_t T, int C, int64_t work, int64_t* len) {
-  const int64_t runs = cdiv(T, C);
-  int64_t n = work > 0 ? 512 / work : 1;
-  if (n > runs / 2) n = runs / 2;
-  if (n < 1) n = 1;
-  *len = cdiv(runs, n) * C;
-  return T > 0 ? (int)cdiv(T, *len) : 1;
-}
 int run_length(int dtype) { return dtype == MDH_BF16 ? 64 : 32; }
-int64_t tiles_of(int da, int dc) { return cdiv(dc, 64 * blocks_of(padded(da), dc)); }
+int64_t tiles_of(int da, int dc) { return cdiv(dc, 64 * blocks_of(padded(da), dc, kVec)); }
 
 }  // namespace
 
@@ -681,9 +712,35 @@ size_t linattn_segment_bytes(int64_t B, int64_t T, int H, int dk, int dv, int dt
   return n > 1 ? (size_t)B * H * n * dk * dv * sizeof(float) * (backward ? 2 : 1) : 0;
 }
 
+// Segments are whole runs.  Their number is that of the least estimated time, in microseconds: a run takes 3.6 where the
+// chip's compute units have a workgroup each, 6 where they have two (more wait for those); with more than one segment
+// their states are summed up first, in 0.6 of that, and each goes through memory four times at 4.5 TB/s.  Sweeps of 1 to 32
+// segments over fifteen sizes: the choice is within some 12 % of the best of them; work to fill the chip twice in every
+// case was up to 17 % off (1 x 2048 x 32 x 128 x 128: 8 segments 52.6 us, 16 60.5; one segment 120).
 int linattn_segments(int64_t B, int64_t T, int H, int dk, int dv, int dtype, bool backward, int64_t* len) {
-  const int64_t work = B * H * (backward ? tiles_of(dv, dk) * 2 + tiles_of(dk, dv) : tiles_of(dk, dv));
-  return segments_of(T, run_length(dtype), work, len);
+  const int C = run_length(dtype);
+  const int64_t runs = cdiv(T, C);
+  // workgroups of the largest launch, for one segment: the passes of d_q and d_k are alike, d_v's may be another kernel
+  const int64_t forward = tiles_of(dk, dv), back = 2 * tiles_of(dv, dk);
+  const bool alike = padded(dk) == padded(dv) && blocks_of(padded(dk), dv, kVec) == blocks_of(padded(dv), dk, kVec);
+  const int64_t work = B * H * (!backward ? forward : alike ? back + forward : back > forward ? back : forward);
+  const double run = (dk > 64 || dv > 64 ? 1.0 : 0.65), state = 4.0 * 4.0 * B * H * dk * dv * (backward ? 2 : 1) / 4.5e6;
+  double best = 0.0;
+  int best_n = 1;
+  *len = (runs < 1 ? 1 : runs) * C;
+  for (int n : {1, 2, 3, 4, 6, 8, 12, 16, 24, 32, 48, 64, 96, 128}) {
+    if (n > 1 && n > runs / 2) break;
+    int64_t each = cdiv(runs, n);
+    // an odd number: segments a power of two apart ask for the same memory channels in step (65536 x 16 x 128 x 128: 452 us
+    // with 32 runs each, 433 with 33)
+    if (n > 1 && each >= 16) each |= 1;
+    const int64_t segs = runs > 0 ? cdiv(runs, each) : 1, groups = work * segs;
+    double t = (double)each * run * (groups <= 256 ? 3.6 : groups <= 512 ? 3.6 + 2.4 * (double)(groups - 256) / 256.0 : 6.0 * (double)groups / 512.0);
+    if (segs > 1) t = 1.6 * t + (double)segs * state + 8.0;
+    if (n == 1 || t < best) best = t, best_n = (int)segs, *len = each * C;
+    if (groups > 1024) break;
+  }
+  return best_n;
 }
 
 // The state entering each of n segments: `p` gives the operands (da x dc = dk x dv).
@@ -692,13 +749,15 @@ mdh_status launch_linattn_segments(const LinattnCall& c, const LinattnPass* p, i
   PassArgs a{};
   a.c = c;
   a.n = np;
-  const int KP = padded(p[0].da), NB = blocks_of(KP, p[0].dc);
+  int access = kVec;
+  for (int i = 0; i < np; ++i) access = access_of(p[i], dtype, false) > access ? access_of(p[i], dtype, false) : access;
+  const int KP = padded(p[0].da), NB = blocks_of(KP, p[0].dc, access);
   for (int i = 0; i < np; ++i) {
     a.p[i] = p[i];
     a.tiles[i] = (int)cdiv(p[i].dc, 64 * NB);
     a.seg[i] = SegmentArgs{n, len, states[i]};
   }
-  mdh_status r = run<true>(a, dtype, KP, NB, st);
+  mdh_status r = run<true>(a, dtype, KP, NB, access, st);
   for (int i = 0; i < np && r == MDH_OK; ++i) {
     const CombineArgs k{c, a.seg[i], p[i].s_in, (int64_t)p[i].da * p[i].dc};
     clear_stale_error();
@@ -714,11 +773,12 @@ mdh_status launch_linattn_pass(const LinattnCall& c, const LinattnPass* passes, 
   bool gone[3] = {};
   for (int i = 0; i < np; ++i) {
     if (gone[i]) continue;
-    const int KP = padded(passes[i].da), NB = blocks_of(KP, passes[i].dc);
+    const int access = access_of(passes[i], dtype, true), KP = padded(passes[i].da), NB = blocks_of(KP, passes[i].dc, access);
     PassArgs a{};
     a.c = c;
     for (int j = i; j < np; ++j) {
-      if (gone[j] || padded(passes[j].da) != KP || blocks_of(KP, passes[j].dc) != NB) continue;
+      if (gone[j] || access_of(passes[j], dtype, true) != access || padded(passes[j].da) != KP || blocks_of(KP, passes[j].dc, access) != NB)
+        continue;
       gone[j] = true;
       a.p[a.n] = passes[j];
       a.tiles[a.n] = (int)cdiv(passes[j].dc, 64 * NB);
@@ -726,7 +786,7 @@ mdh_status launch_linattn_pass(const LinattnCall& c, const LinattnPass* passes, 
       a.seg_t[a.n] = turned[j];
       ++a.n;
     }
-    const mdh_status r = run<false>(a, dtype, KP, NB, st);
+    const mdh_status r = run<false>(a, dtype, KP, NB, access, st);
     if (r != MDH_OK) return r;
   }
   return MDH_OK;
