@@ -7,7 +7,9 @@ computation runs inside the library's kernels.
 from __future__ import annotations
 
 import ctypes
+import math
 import os
+import struct
 from typing import Optional, Sequence
 
 HERE = os.path.dirname(os.path.abspath(__file__))
@@ -163,15 +165,16 @@ def lib() -> ctypes.CDLL:
         L.mdh_calib_valu_kind.argtypes = [i32, vp, vp, i32, p64, vp, vp]
         L.mdh_calib_realtime_hz.restype = i64
         L.mdh_calib_realtime_hz.argtypes = []
+        packed = vp  # int64 one after the other: bytes, or an array
         L.mdh_linattn_workspace_size.restype = sz
-        L.mdh_linattn_workspace_size.argtypes = [p64, ctypes.c_int, i32]
-        L.mdh_linattn.argtypes = [p64, ctypes.c_int, vp, vp, vp, p64, vp, f32, vp, vp, vp, vp, i64, vp, vp, sz, vp]
-        L.mdh_linattn_backward.argtypes = [p64, ctypes.c_int, vp, vp, vp, vp, p64, vp, f32, vp, vp, vp, vp, vp, vp, vp, vp, sz, vp]
-        L.mdh_linattn_step.argtypes = [p64, ctypes.c_int, vp, vp, vp, p64, vp, f32, vp, vp, i64, vp, vp]
+        L.mdh_linattn_workspace_size.argtypes = [packed, ctypes.c_int, i32]
+        L.mdh_linattn.argtypes = [packed, ctypes.c_int, vp, vp, vp, packed, vp, f32, vp, vp, vp, vp, i64, vp, vp, sz, vp]
+        L.mdh_linattn_backward.argtypes = [packed, ctypes.c_int, vp, vp, vp, vp, packed, vp, f32, vp, vp, vp, vp, vp, vp, vp, vp, sz, vp]
+        L.mdh_linattn_step.argtypes = [packed, ctypes.c_int, vp, vp, vp, packed, vp, f32, vp, vp, i64, vp, vp]
         L.mdh_group_norm_workspace_size.restype = sz
-        L.mdh_group_norm_workspace_size.argtypes = [p64, ctypes.c_int, i32]
-        L.mdh_group_norm.argtypes = [p64, ctypes.c_int, vp, vp, p64, vp, vp, f32, i32, vp, vp, vp, vp, sz, vp]
-        L.mdh_group_norm_backward.argtypes = [p64, ctypes.c_int, vp, vp, vp, p64, vp, vp, vp, vp, i32, vp, vp, vp, vp, vp, sz, vp]
+        L.mdh_group_norm_workspace_size.argtypes = [packed, ctypes.c_int, i32]
+        L.mdh_group_norm.argtypes = [packed, ctypes.c_int, vp, vp, packed, vp, vp, f32, i32, vp, vp, vp, vp, sz, vp]
+        L.mdh_group_norm_backward.argtypes = [packed, ctypes.c_int, vp, vp, vp, packed, vp, vp, vp, vp, i32, vp, vp, vp, vp, vp, sz, vp]
         L.mdh_num_candidates.restype = i32
         L.mdh_num_candidates.argtypes = [ctypes.c_int, p64]
         L.mdh_candidate.argtypes = [ctypes.c_int, p64, i32, pp]
@@ -401,18 +404,26 @@ def mdh_matvec(A, x, y, params: Optional[TileParams] = None, workspace=None):
 
 
 # ------------------------------------------------------------------ sequence layers
+#
+# Sizes and strides cross the ABI as bytes of int64: packing them takes a fifth of the time that filling a ctypes array does,
+# and a token's group norm or step is as fast as the host is (of 10 us a call 4 are left).
+
+_q4, _q7, _q8 = (struct.Struct("%dq" % n).pack for n in (4, 7, 8))
 
 
 def _dtype_of(dtype) -> int:
-    lib()
-    if dtype not in _DTYPES:
+    d = _DTYPES.get(dtype)
+    if d is None and _lib is None:
+        lib()  # (fills the table)
+        d = _DTYPES.get(dtype)
+    if d is None:
         raise TypeError("float32 or bfloat16 is required, not %s" % dtype)
-    return _DTYPES[dtype]
+    return d
 
 
 def _strided(t, dtype, name):
     """A tensor on the GPU whose channels are adjacent; its other strides are its own."""
-    if isinstance(t, _Tensor) and t.is_cuda and t.dtype == dtype and (t.stride(-1) == 1 or t.shape[-1] == 1):
+    if isinstance(t, _Tensor) and t.is_cuda and t.dtype == dtype and (t.is_contiguous() or t.stride(-1) == 1 or t.shape[-1] == 1):
         return t.data_ptr()
     raise TypeError("%s must be a %s tensor on the GPU with adjacent channels" % (name, dtype))
 
@@ -420,16 +431,18 @@ def _strided(t, dtype, name):
 def _opt(t, dtype, name, shape=None):
     if t is None:
         return None
-    if shape is not None and tuple(t.shape) != shape:
+    if shape is not None and t.shape != shape:
         raise ValueError("%s has shape %s, not %s" % (name, tuple(t.shape), shape))
     return _dev(t, dtype, name)
 
 
 def _strides(tensors):
     """All but the channels' strides, one tensor after the other; None where all are dense."""
-    if all(t.is_contiguous() for t in tensors):
-        return None
-    return _sizes([s for t in tensors for s in t.stride()[:-1]])
+    for t in tensors:
+        if not t.is_contiguous():
+            s = [n for u in tensors for n in u.stride()[:-1]]
+            return struct.pack("%dq" % len(s), *s)
+    return None
 
 
 def _states(B, H, dk, dv, slots, *named):
@@ -439,13 +452,17 @@ def _states(B, H, dk, dv, slots, *named):
         n = max((t.shape[0] for t, _ in named if t is not None), default=0)
         if any(t is not None and t.shape[0] != n for t, _ in named):
             raise ValueError("the pools of states have different numbers of slots")
-    got = [_opt(t, _F32, name, (B if slots is None else n, H, dk, dv)) for t, name in named]
-    return got, n, _opt(slots, _I32, "slots", (B,))
+    shape = (B if slots is None else n, H, dk, dv)
+    return [_opt(t, _F32, name, shape) for t, name in named], n, _opt(slots, _I32, "slots", (B,))
+
+
+def _unfit(*named):
+    return ValueError("shapes do not fit: " + ", ".join("%s %s" % (name, tuple(t.shape)) for name, t in named))
 
 
 def mdh_linattn_workspace_size(sizes: Sequence[int], dtype, backward: bool = False) -> int:
     """``sizes``: (B, T, H, Hq, Hk, Hv, dk, dv); ``dtype``: torch.float32 or torch.bfloat16."""
-    return int(lib().mdh_linattn_workspace_size(_sizes(sizes), _dtype_of(dtype), int(backward)))
+    return int(lib().mdh_linattn_workspace_size(_q8(*sizes), _dtype_of(dtype), int(backward)))
 
 
 def mdh_linattn(q, k, v, log_decay, o, scale: float = 1.0, lengths=None, initial_state=None, final_state=None, slots=None,
@@ -454,16 +471,16 @@ def mdh_linattn(q, k, v, log_decay, o, scale: float = 1.0, lengths=None, initial
 
     q: (B, T, Hq, dk), k: (B, T, Hk, dk), v: (B, T, Hv, dv), o: (B, T, H, dv), any strides with adjacent channels; log_decay: (H,);
     lengths: (B,) int32; states: (B, H, dk, dv) float32, or with slots (B,) int32 pools (n, H, dk, dv)."""
-    L = lib()
+    L = _lib or lib()
     B, T, Hq, dk = q.shape
-    H, dv = o.shape[2], o.shape[3]
+    _, _, H, dv = shape = o.shape
     Hk, Hv = k.shape[2], v.shape[2]
-    if k.shape != (B, T, Hk, dk) or v.shape != (B, T, Hv, dv) or o.shape[:2] != (B, T):
-        raise ValueError("shapes of q, k, v and o do not fit: %s %s %s %s" % (*(tuple(t.shape) for t in (q, k, v, o)),))
+    if k.shape != (B, T, Hk, dk) or v.shape != (B, T, Hv, dv) or shape != (B, T, H, dv):
+        raise _unfit(("q", q), ("k", k), ("v", v), ("o", o))
     dt = q.dtype
     states, n, slots_p = _states(B, H, dk, dv, slots, (initial_state, "initial_state"), (final_state, "final_state"))
     wp, wb = _ws(workspace)
-    st = L.mdh_linattn(_sizes((B, T, H, Hq, Hk, Hv, dk, dv)), _dtype_of(dt), _strided(q, dt, "q"), _strided(k, dt, "k"),
+    st = L.mdh_linattn(_q8(B, T, H, Hq, Hk, Hv, dk, dv), _dtype_of(dt), _strided(q, dt, "q"), _strided(k, dt, "k"),
                        _strided(v, dt, "v"), _strides((q, k, v, o)), _opt(log_decay, _F32, "log_decay", (H,)), scale,
                        _opt(lengths, _I32, "lengths", (B,)), states[0], states[1], slots_p, n, _strided(o, dt, "o"), wp, wb, _stream())
     _check(st, "mdh_linattn")
@@ -473,19 +490,19 @@ def mdh_linattn(q, k, v, log_decay, o, scale: float = 1.0, lengths=None, initial
 def mdh_linattn_backward(q, k, v, log_decay, d_o, d_q, d_k, d_v, scale: float = 1.0, lengths=None, initial_state=None,
                          d_final_state=None, d_initial_state=None, workspace=None):
     """Gradients of mdh_linattn for q, k, v and the initial state, from those of o and of the final state."""
-    L = lib()
+    L = _lib or lib()
     B, T, Hq, dk = q.shape
     H, dv = d_o.shape[2], d_o.shape[3]
     Hk, Hv = k.shape[2], v.shape[2]
-    if k.shape != (B, T, Hk, dk) or v.shape != (B, T, Hv, dv) or d_o.shape[:2] != (B, T):
-        raise ValueError("shapes of q, k, v and d_o do not fit: %s %s %s %s" % (*(tuple(t.shape) for t in (q, k, v, d_o)),))
+    if k.shape != (B, T, Hk, dk) or v.shape != (B, T, Hv, dv) or d_o.shape != (B, T, H, dv):
+        raise _unfit(("q", q), ("k", k), ("v", v), ("d_o", d_o))
     if d_q.shape != q.shape or d_k.shape != k.shape or d_v.shape != v.shape:
         raise ValueError("a gradient has the shape of what it is the gradient of")
     dt = q.dtype
     states, _, _ = _states(B, H, dk, dv, None, (initial_state, "initial_state"), (d_final_state, "d_final_state"),
                            (d_initial_state, "d_initial_state"))
     wp, wb = _ws(workspace)
-    st = L.mdh_linattn_backward(_sizes((B, T, H, Hq, Hk, Hv, dk, dv)), _dtype_of(dt), _strided(q, dt, "q"), _strided(k, dt, "k"),
+    st = L.mdh_linattn_backward(_q8(B, T, H, Hq, Hk, Hv, dk, dv), _dtype_of(dt), _strided(q, dt, "q"), _strided(k, dt, "k"),
                                 _strided(v, dt, "v"), _strided(d_o, dt, "d_o"), _strides((q, k, v, d_o, d_q, d_k, d_v)),
                                 _opt(log_decay, _F32, "log_decay", (H,)), scale, _opt(lengths, _I32, "lengths", (B,)), states[0],
                                 states[1], _strided(d_q, dt, "d_q"), _strided(d_k, dt, "d_k"), _strided(d_v, dt, "d_v"), states[2],
@@ -497,15 +514,16 @@ def mdh_linattn_backward(q, k, v, log_decay, d_o, d_q, d_k, d_v, scale: float = 
 def mdh_linattn_step(q, k, v, log_decay, state, o, scale: float = 1.0, slots=None):
     """One token with the state in place.  q: (B, Hq, dk), k: (B, Hk, dk), v: (B, Hv, dv), o: (B, H, dv);
     state: (B, H, dk, dv) float32, or with slots (B,) int32 a pool (n, H, dk, dv)."""
-    L = lib()
+    L = _lib or lib()
     B, Hq, dk = q.shape
-    H, dv = o.shape[1], o.shape[2]
-    Hk, Hv = k.shape[1], v.shape[1]
-    if k.shape != (B, Hk, dk) or v.shape != (B, Hv, dv) or o.shape[0] != B:
-        raise ValueError("shapes of q, k, v and o do not fit: %s %s %s %s" % (*(tuple(t.shape) for t in (q, k, v, o)),))
+    _, H, dv = shape = o.shape
+    _, Hk, dk2 = k.shape
+    B3, Hv, dv3 = v.shape
+    if k.shape[0] != B or dk2 != dk or B3 != B or dv3 != dv or shape[0] != B:
+        raise _unfit(("q", q), ("k", k), ("v", v), ("o", o))
     dt = q.dtype
     (state_p,), n, slots_p = _states(B, H, dk, dv, slots, (state, "state"))
-    st = L.mdh_linattn_step(_sizes((B, H, Hq, Hk, Hv, dk, dv)), _dtype_of(dt), _strided(q, dt, "q"), _strided(k, dt, "k"),
+    st = L.mdh_linattn_step(_q7(B, H, Hq, Hk, Hv, dk, dv), _dtype_of(dt), _strided(q, dt, "q"), _strided(k, dt, "k"),
                             _strided(v, dt, "v"), _strides((q, k, v, o)), _opt(log_decay, _F32, "log_decay", (H,)), scale, state_p,
                             slots_p, n, _strided(o, dt, "o"), _stream())
     _check(st, "mdh_linattn_step")
@@ -514,13 +532,15 @@ def mdh_linattn_step(q, k, v, log_decay, state, o, scale: float = 1.0, slots=Non
 
 def _rows(t, name, shape, dtype):
     """(pointer, elements from row to row) of a tensor (N, ..., C) whose positions are evenly spaced."""
+    if t is None:
+        return None, 0
     if t.shape != shape:
         raise ValueError("%s has shape %s, not %s" % (name, tuple(t.shape), tuple(shape)))
     p = _strided(t, dtype, name)
     if t.is_contiguous():
-        return p, t.shape[-1]
+        return p, shape[-1]
     step, per = 0, 1  # from the last position's dimension outwards
-    for n, s in zip(reversed(t.shape[:-1]), reversed(t.stride()[:-1])):
+    for n, s in zip(reversed(shape[:-1]), reversed(t.stride()[:-1])):
         if n == 1:
             continue
         if per == 1:
@@ -531,31 +551,26 @@ def _rows(t, name, shape, dtype):
     return p, step
 
 
-def _positions(shape):
-    S = 1
-    for n in shape[1:-1]:
-        S *= n
-    return shape[0], S, shape[-1]
-
-
 def mdh_group_norm_workspace_size(sizes: Sequence[int], dtype, backward: bool = False) -> int:
     """``sizes``: (N, S, C, G); ``dtype``: torch.float32 or torch.bfloat16."""
-    return int(lib().mdh_group_norm_workspace_size(_sizes(sizes), _dtype_of(dtype), int(backward)))
+    return int(lib().mdh_group_norm_workspace_size(_q4(*sizes), _dtype_of(dtype), int(backward)))
 
 
 def mdh_group_norm(x, weight, bias, y, groups: int, eps: float = 1e-5, act: int = MDH_ACT_NONE, gate=None, mean=None, rstd=None,
                    workspace=None):
     """y = act(z), or z * act(gate), with z the group norm of x: (N, C) or (N, positions..., C), channels last.
     weight, bias: (C,) float32 or None; mean, rstd: (N, groups) float32 or None, what the backward call wants."""
-    L = lib()
-    N, S, C = _positions(x.shape)
+    L = _lib or lib()
+    shape = x.shape
+    N, C = shape[0], shape[-1]
     dt = x.dtype
-    (xp, xs), (yp, ys) = _rows(x, "x", x.shape, dt), _rows(y, "y", x.shape, dt)
-    gp, gs = _rows(gate, "gate", x.shape, dt) if gate is not None else (None, 0)
+    d = _dtype_of(dt)
+    (xp, xs), (yp, ys), (gp, gs) = _rows(x, "x", shape, dt), _rows(y, "y", shape, dt), _rows(gate, "gate", shape, dt)
     wp, wb = _ws(workspace)
-    st = L.mdh_group_norm(_sizes((N, S, C, groups)), _dtype_of(dt), xp, gp, _sizes((xs, gs, ys)), _opt(weight, _F32, "weight", (C,)),
-                          _opt(bias, _F32, "bias", (C,)), eps, act, yp, _opt(mean, _F32, "mean", (N, groups)),
-                          _opt(rstd, _F32, "rstd", (N, groups)), wp, wb, _stream())
+    st = L.mdh_group_norm(_q4(N, math.prod(shape[1:-1]), C, groups), d, xp, gp,
+                          None if xs == ys == C and (gp is None or gs == C) else struct.pack("3q", xs, gs, ys),
+                          _opt(weight, _F32, "weight", (C,)), _opt(bias, _F32, "bias", (C,)), eps, act, yp,
+                          _opt(mean, _F32, "mean", (N, groups)), _opt(rstd, _F32, "rstd", (N, groups)), wp, wb, _stream())
     _check(st, "mdh_group_norm")
     return y
 
@@ -563,15 +578,17 @@ def mdh_group_norm(x, weight, bias, y, groups: int, eps: float = 1e-5, act: int 
 def mdh_group_norm_backward(x, weight, bias, mean, rstd, d_y, d_x, d_weight, d_bias, groups: int, act: int = MDH_ACT_NONE, gate=None,
                             d_gate=None, workspace=None):
     """Gradients of mdh_group_norm, whose mean and rstd it takes; d_weight, d_bias: (C,) float32 or None."""
-    L = lib()
-    N, S, C = _positions(x.shape)
+    L = _lib or lib()
+    shape = x.shape
+    N, C = shape[0], shape[-1]
     dt = x.dtype
+    d = _dtype_of(dt)
     if (gate is None) != (d_gate is None):
         raise ValueError("d_gate goes with gate")
-    (xp, xs), (yp, ys), (dxp, dxs) = (_rows(t, n, x.shape, dt) for t, n in ((x, "x"), (d_y, "d_y"), (d_x, "d_x")))
-    (gp, gs), (dgp, dgs) = (_rows(t, n, x.shape, dt) if t is not None else (None, 0) for t, n in ((gate, "gate"), (d_gate, "d_gate")))
+    named = ((x, "x"), (gate, "gate"), (d_y, "d_y"), (d_x, "d_x"), (d_gate, "d_gate"))
+    (xp, xs), (gp, gs), (yp, ys), (dxp, dxs), (dgp, dgs) = (_rows(t, name, shape, dt) for t, name in named)
     wp, wb = _ws(workspace)
-    st = L.mdh_group_norm_backward(_sizes((N, S, C, groups)), _dtype_of(dt), xp, gp, yp, _sizes((xs, gs, ys, dxs, dgs)),
+    st = L.mdh_group_norm_backward(_q4(N, math.prod(shape[1:-1]), C, groups), d, xp, gp, yp, struct.pack("5q", xs, gs, ys, dxs, dgs),
                                    _opt(weight, _F32, "weight", (C,)), _opt(bias, _F32, "bias", (C,)),
                                    _opt(mean, _F32, "mean", (N, groups)), _opt(rstd, _F32, "rstd", (N, groups)), act, dxp, dgp,
                                    _opt(d_weight, _F32, "d_weight", (C,)), _opt(d_bias, _F32, "d_bias", (C,)), wp, wb, _stream())
