@@ -537,19 +537,22 @@ __global__ __launch_bounds__(kThreads, ACCESS == kEach ? 2 : KP == 64 && NB == 1
       const __amdgpu_buffer_rsrc_t to = rsrc_of(out_base + (int64_t)(rev ? len - pos - C : pos) * out_pitch);
 #pragma unroll
       for (int i = 0; i < TB; ++i) {
-        const int step = (rev ? TB - 1 - i : i) * 16 * out_pitch;
+        // The whole distance is in the vector register: with a scalar offset beside it, a 16-byte store was seen to take its first
+        // words from after the next write to their registers (lanes 12 to 15 of 16, with the chip loaded), which the compiler
+        // guards against without one only.
+        const int out_i = out_at + (rev ? TB - 1 - i : i) * 16 * out_pitch;
         const bool there = 16 * i + l16 < n;
         if (p.out_f32 || sizeof(T) == 4) {
 #pragma unroll
           for (int nb = 0; nb < NB; ++nb) {
-            const int c = out_col + 4 * nb, to_c = out_at + 16 * nb;
+            const int c = out_col + 4 * nb, to_c = out_i + 16 * nb;
             const bool whole = ACCESS == kVec ? c < dc : c + 4 <= dc;  // (rows of fp32 partial sums: their own multiple of 4)
-            __builtin_amdgcn_raw_buffer_store_b128(__builtin_bit_cast(u4, out[i][nb]), to, there && whole ? to_c : kPast, step, 0);
+            __builtin_amdgcn_raw_buffer_store_b128(__builtin_bit_cast(u4, out[i][nb]), to, there && whole ? to_c : kPast, 0, 0);
             if (ACCESS != kVec)
 #pragma unroll
               for (int e = 0; e < 3; ++e)
                 __builtin_amdgcn_raw_buffer_store_b32(__float_as_uint(out[i][nb][e]), to,
-                                                      there && !whole && c + e < dc ? to_c + 4 * e : kPast, step, 0);
+                                                      there && !whole && c + e < dc ? to_c + 4 * e : kPast, 0, 0);
           }
         } else {
           uint32_t w[2 * NB];
@@ -560,14 +563,14 @@ __global__ __launch_bounds__(kThreads, ACCESS == kEach ? 2 : KP == 64 && NB == 1
           }
           const bool whole = ACCESS == kVec ? out_col < dc : out_col + 4 * NB <= dc;
           if constexpr (NB == 2)
-            __builtin_amdgcn_raw_buffer_store_b128((u4){w[0], w[1], w[2], w[3]}, to, there && whole ? out_at : kPast, step, 0);
+            __builtin_amdgcn_raw_buffer_store_b128((u4){w[0], w[1], w[2], w[3]}, to, there && whole ? out_i : kPast, 0, 0);
           else
-            __builtin_amdgcn_raw_buffer_store_b64((u2){w[0], w[1]}, to, there && whole ? out_at : kPast, step, 0);
+            __builtin_amdgcn_raw_buffer_store_b64((u2){w[0], w[1]}, to, there && whole ? out_i : kPast, 0, 0);
           if (ACCESS != kVec)
 #pragma unroll
             for (int e = 0; e < 4 * NB - 1; ++e)
               __builtin_amdgcn_raw_buffer_store_b16((uint16_t)(w[e / 2] >> (16 * (e & 1))), to,
-                                                    there && !whole && out_col + e < dc ? out_at + 2 * e : kPast, step, 0);
+                                                    there && !whole && out_col + e < dc ? out_i + 2 * e : kPast, 0, 0);
         }
       }
     }

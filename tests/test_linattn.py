@@ -346,6 +346,36 @@ def test_same_bits_on_another_stream_and_in_a_graph():
         assert same()
 
 
+def _pairs(p, magnitude):
+    """o and the gradients in 64 bits on the GPU, from the products of all pairs of tokens (no shared heads, no states)."""
+    f = torch.abs if magnitude else (lambda t: t)
+    q, k, v, d_o = (f(t.cuda().double()).transpose(1, 2).contiguous() for t in (p.q, p.k, p.v, p.d_o))
+    i = torch.arange(p.T, device="cuda")
+    near = torch.where(i[:, None] >= i, torch.exp(p.g.cuda().double()[:, None, None] * (i[:, None] - i).clamp_min(0)), 0.0) * p.scale
+    scores, d_scores = (q @ k.transpose(2, 3).contiguous()) * near, (d_o @ v.transpose(2, 3).contiguous()) * near
+    turn = lambda t: t.transpose(2, 3).contiguous()  # noqa: E731
+    got = scores @ v, d_scores @ k, turn(d_scores) @ q, turn(scores) @ d_o
+    return [t.transpose(1, 2) for t in got]
+
+
+@gpu
+@pytest.mark.parametrize("dtype", [F32, BF16])
+@pytest.mark.parametrize("B,T,H,dk,dv", [(4, 1024, 16, 128, 128), (4, 1000, 16, 100, 90), (8, 512, 16, 64, 64), (2, 1024, 16, 64, 128),
+                                         (4, 512, 12, 192, 256), (6, 700, 16, 63, 33)])
+def test_chip_full_of_work(dtype, B, T, H, dk, dv):
+    """Every output, with every compute unit busy: three calls in a row, each compared."""
+    p = Problem(dtype, B, T, H, dk, dv, states=False)
+    ref, mag = _pairs(p, False), _pairs(p, True)
+    n = dk + dv + 2 * T + 32
+    for _ in range(3):
+        o, _ = p.forward()
+        for got, r, m, what in zip((o, *p.backward()[:3]), ref, mag, ("o", "d_q", "d_k", "d_v")):
+            limit = ((2.0 ** -7 if dtype == BF16 else 0) + n * U) * m + 1e-37
+            off = (got.double() - r).abs()
+            assert (off <= limit).all(), "%s: %.2f times its limit, %d outputs" % (what, (off / limit).max(), int((off > limit).sum()))
+            assert off.square().mean().sqrt() <= (2.0 ** -7 if dtype == BF16 else 2.0 ** -20) * r.square().mean().sqrt(), what
+
+
 # ------------------------------------------------------------------ refusals: nothing is launched
 
 
