@@ -612,15 +612,17 @@ __global__ __launch_bounds__(kThreads, ACCESS == kEach ? 2 : KP == 64 && NB == 1
 }
 
 // Prefix sum over the segments: what is in segment g's place is the sum of segment g - 1 alone; after it, the state that
-// enters g.  One thread for each element of each (b, h).
+// enters g.  One thread for V elements of each (b, h): bound by the states' way to memory and back.
 struct CombineArgs {
   LinattnCall c;
   SegmentArgs seg;
   const float* s_in;
   int64_t elems;
 };
+template <int V>
 __global__ __launch_bounds__(256) void linattn_segments_kernel(CombineArgs a) {
-  const int64_t e = (int64_t)blockIdx.y * 256 + threadIdx.x;
+  typedef float fv __attribute__((ext_vector_type(V)));
+  const int64_t e = ((int64_t)blockIdx.y * 256 + threadIdx.x) * V;
   if (e >= a.elems) return;
   const int64_t bh = blockIdx.x, b = bh / a.c.H;
   const int h = (int)(bh % a.c.H);
@@ -628,33 +630,40 @@ __global__ __launch_bounds__(256) void linattn_segments_kernel(CombineArgs a) {
   const float log_decay = a.c.log_decay[h];
   const Decay full = decay_power(log_decay, a.seg.len);
   float* s = a.seg.states + bh * a.seg.n * a.elems + e;
-  float run = a.s_in && slot >= 0 ? a.s_in[(slot * a.c.H + h) * a.elems + e] : 0.f;
-  if (a.s_in) s[0] = run;
+  fv run = {};
+  if (a.s_in && slot >= 0) run = *(const fv*)(a.s_in + (slot * a.c.H + h) * a.elems + e);
+  if (a.s_in) *(fv*)s = run;
   constexpr int U = 8;
   for (int g0 = 1; g0 < a.seg.n; g0 += U) {
-    float x[U];
+    fv x[U];
 #pragma unroll
-    for (int u = 0; u < U; ++u) x[u] = g0 + u < a.seg.n ? s[(g0 + u) * a.elems] : 0.f;
+    for (int u = 0; u < U; ++u)
+      if (g0 + u < a.seg.n) x[u] = *(const fv*)(s + (g0 + u) * a.elems);
 #pragma unroll
     for (int u = 0; u < U; ++u)
       if (g0 + u < a.seg.n) {
         const int64_t n = min(max(len - (g0 + u - 1) * a.seg.len, (int64_t)0), a.seg.len);  // positions of the segment before
-        run = (n == a.seg.len ? full : decay_power(log_decay, n)) * run + x[u];
-        s[(g0 + u) * a.elems] = run;
+        const Decay d = n == a.seg.len ? full : decay_power(log_decay, n);
+#pragma unroll
+        for (int i = 0; i < V; ++i) run[i] = d * run[i] + x[u][i];
+        *(fv*)(s + (g0 + u) * a.elems) = run;
       }
   }
 }
 
+// Gradients of shared heads: a workgroup for each token, a lane for the channels that are 256 apart.
 template <typename T>
-__global__ __launch_bounds__(256) void linattn_share_kernel(const float* __restrict__ src, HeadView dst, int64_t T_, int H, int heads,
-                                                            int d, int64_t total) {
-  const int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x;  // (b, t, shared head, channel)
-  if (i >= total) return;
-  const int ch = (int)(i % d), g = H / heads;
-  const int64_t r = i / d, hs = r % heads, bt = r / heads;
-  float sum = 0.f;
-  for (int j = 0; j < g; ++j) sum += src[(bt * H + hs * g + j) * d + ch];
-  ((T*)dst.p)[bt / T_ * dst.sb + bt % T_ * dst.st + hs * dst.sh + ch] = from_float<T>(sum);
+__global__ __launch_bounds__(256) void linattn_share_kernel(const float* __restrict__ src, HeadView dst, int T_, int H, int heads, int d) {
+  const int64_t bt = blockIdx.x;
+  const int g = H / heads;
+  const float* from = src + bt * H * d;
+  T* to = (T*)dst.p + bt / T_ * dst.sb + bt % T_ * dst.st;
+  for (int e = threadIdx.x; e < heads * d; e += 256) {
+    const int hs = e / d, ch = e % d;
+    float sum = 0.f;
+    for (int j = 0; j < g; ++j) sum += from[(int64_t)(hs * g + j) * d + ch];
+    to[hs * dst.sh + ch] = from_float<T>(sum);
+  }
 }
 
 template <typename T, int KP, int NB, bool STATE, int ACCESS>
@@ -764,7 +773,11 @@ mdh_status launch_linattn_segments(const LinattnCall& c, const LinattnPass* p, i
   for (int i = 0; i < np && r == MDH_OK; ++i) {
     const CombineArgs k{c, a.seg[i], p[i].s_in, (int64_t)p[i].da * p[i].dc};
     clear_stale_error();
-    linattn_segments_kernel<<<dim3((unsigned)(c.B * c.H), (unsigned)cdiv(k.elems, 256)), 256, 0, st>>>(k);
+    const unsigned states_n = (unsigned)(c.B * c.H);
+    if (k.elems % 4 == 0)  // (the states are 16-byte aligned)
+      linattn_segments_kernel<4><<<dim3(states_n, (unsigned)cdiv(k.elems, 1024)), 256, 0, st>>>(k);
+    else
+      linattn_segments_kernel<1><<<dim3(states_n, (unsigned)cdiv(k.elems, 256)), 256, 0, st>>>(k);
     r = launch_status();
   }
   return r;
@@ -797,15 +810,14 @@ mdh_status launch_linattn_pass(const LinattnCall& c, const LinattnPass* passes, 
 
 mdh_status launch_linattn_share(const LinattnCall& c, const float* src, int d, const HeadView& dst, int heads, int dtype,
                                 hipStream_t st) {
-  const int64_t total = c.B * c.T * heads * d;
-  if (total == 0) return MDH_OK;
-  const int64_t blocks = cdiv(total, 256);
-  if (blocks > 0x7fffffff) return MDH_ERR_SIZE;
+  const int64_t tokens = c.B * c.T;
+  if (tokens == 0) return MDH_OK;
+  if (tokens > 0x7fffffff) return MDH_ERR_SIZE;
   clear_stale_error();
   if (dtype == MDH_BF16)
-    linattn_share_kernel<bf16><<<dim3((unsigned)blocks), 256, 0, st>>>(src, dst, c.T, c.H, heads, d, total);
+    linattn_share_kernel<bf16><<<dim3((unsigned)tokens), 256, 0, st>>>(src, dst, (int)c.T, c.H, heads, d);
   else
-    linattn_share_kernel<float><<<dim3((unsigned)blocks), 256, 0, st>>>(src, dst, c.T, c.H, heads, d, total);
+    linattn_share_kernel<float><<<dim3((unsigned)tokens), 256, 0, st>>>(src, dst, (int)c.T, c.H, heads, d);
   return launch_status();
 }
 
