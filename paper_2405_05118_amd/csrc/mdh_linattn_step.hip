@@ -1,16 +1,16 @@
 // One token of linear attention, the state in place: state <- l state + k v^T, o = scale state^T q.
 //
 // 2 * dk * dv multiply-adds on dk * dv numbers that are read and written once: bound by the memory that holds the states,
-// or, with few of them, by one trip to it.  A workgroup owns W columns of one state (whole rows where there are states
-// enough to fill the chip, 16 columns where not), a lane 4 columns of every 1024/W-th row: the sum over the rows that q
-// asks for stays in the workgroup.
+// or, with few of them, by one trip to it.  A workgroup owns W columns of one state, a lane 4 columns
+// of every 1024/W-th row: the sum over the rows that q asks for stays in the workgroup.  A lane's first eight loads are
+// under way before anything is waited for.  W is 64 where that gives the chip two workgroups a compute unit, else 16.
+// Measured in a graph, W = 128 / 64 / 16, states of 128 x 128: 32 of them 8.6 / 5.4 / 4.4 us, 128 12.4 / 8.2 / 7.9, 256
+// 14.8 / 10.8 / 12.9, 1024 33 / 32 / 40, 4096 117 / 112 / 164 (4.8 TB/s); of 64 x 64: 512 7.9 / 7.4 / 9.6.
 #include "mdh_internal.h"
 #include "mdh_types.h"
 
 namespace mdh {
 namespace {
-
-typedef float f4 __attribute__((ext_vector_type(4)));
 
 struct StepArgs {
   LinattnCall c;
@@ -24,6 +24,7 @@ struct StepArgs {
 template <typename T, int V, int LW>
 __global__ __launch_bounds__(256) void linattn_step_kernel(StepArgs s) {
   constexpr int RP = 256 / LW;  // rows at once
+  typedef float fv __attribute__((ext_vector_type(V)));
   __shared__ float ks[256], qs[256], red[256 / 64][V * LW];
   const int h = blockIdx.x % s.c.H;
   const int64_t b = blockIdx.x / s.c.H;
@@ -38,11 +39,15 @@ __global__ __launch_bounds__(256) void linattn_step_kernel(StepArgs s) {
         if (col + e < s.dv) o[col + e] = from_float<T>(0.f);
     return;
   }
-  const Decay l = decay_power(s.c.log_decay[h], 1);
-  if ((int)threadIdx.x < s.dk) {
-    ks[threadIdx.x] = to_float(((const T*)s.k.p + b * s.k.sb + (h / s.k.group) * s.k.sh)[threadIdx.x]);
-    qs[threadIdx.x] = to_float(((const T*)s.q.p + b * s.q.sb + (h / s.q.group) * s.q.sh)[threadIdx.x]);
-  }
+  constexpr int U = 8;
+  float* st = s.state + ((slot * s.c.H + h) * s.dk) * (int64_t)s.dv + col;
+  fv x[U];
+  auto read = [&](int r0) {
+#pragma unroll
+    for (int u = 0; u < U; ++u)
+      if (col < s.dv && r0 + u * RP < s.dk) x[u] = *(const fv*)(st + (int64_t)(r0 + u * RP) * s.dv);
+  };
+  read(row);
   const T* pv = (const T*)s.v.p + b * s.v.sb + (h / s.v.group) * s.v.sh;
   float v[V], sum[V];
 #pragma unroll
@@ -50,29 +55,25 @@ __global__ __launch_bounds__(256) void linattn_step_kernel(StepArgs s) {
     v[e] = col + e < s.dv ? to_float(pv[col + e]) : 0.f;
     sum[e] = 0.f;
   }
+  if ((int)threadIdx.x < s.dk) {
+    ks[threadIdx.x] = to_float(((const T*)s.k.p + b * s.k.sb + (h / s.k.group) * s.k.sh)[threadIdx.x]);
+    qs[threadIdx.x] = to_float(((const T*)s.q.p + b * s.q.sb + (h / s.q.group) * s.q.sh)[threadIdx.x]);
+  }
+  const Decay l = decay_power(s.c.log_decay[h], 1);
   __syncthreads();
-  float* st = s.state + ((slot * s.c.H + h) * s.dk) * (int64_t)s.dv + col;
-  if (col < s.dv) {
-#pragma unroll 8
-    for (int r = row; r < s.dk; r += RP) {
-      float* at = st + (int64_t)r * s.dv;
-      float x[V];
-      if constexpr (V == 4) {
-        const f4 w = *(const f4*)at;
-        for (int e = 0; e < 4; ++e) x[e] = w[e];
-      } else {
-        x[0] = at[0];
-      }
+  for (int r0 = row; r0 < s.dk; r0 += U * RP) {
+    if (r0 != row) read(r0);
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+      const int r = r0 + u * RP;
+      if (col >= s.dv || r >= s.dk) continue;
       const float kr = ks[r], qr = qs[r];
 #pragma unroll
       for (int e = 0; e < V; ++e) {
-        x[e] = l * x[e] + kr * v[e];
-        sum[e] += qr * x[e];
+        x[u][e] = l * x[u][e] + kr * v[e];
+        sum[e] += qr * x[u][e];
       }
-      if constexpr (V == 4)
-        *(f4*)at = (f4){x[0], x[1], x[2], x[3]};
-      else
-        at[0] = x[0];
+      *(fv*)(st + (int64_t)r * s.dv) = x[u];
     }
   }
   // rows: over the lanes of a wavefront that share columns, then over the wavefronts
@@ -96,9 +97,11 @@ void step(const StepArgs& s, bool vec, hipStream_t st) {
   const unsigned states = (unsigned)(s.c.B * s.c.H);
   auto grid = [&](int w) { return dim3(states, (s.dv + w - 1) / w); };
   if (!vec)
-    linattn_step_kernel<T, 1, 64><<<grid(64), 256, 0, st>>>(s);
+    linattn_step_kernel<T, 1, 16><<<grid(16), 256, 0, st>>>(s);
+  else if ((int64_t)states * ((s.dv + 63) / 64) >= 512)
+    linattn_step_kernel<T, 4, 16><<<grid(64), 256, 0, st>>>(s);
   else
-    linattn_step_kernel<T, 4, 32><<<grid(128), 256, 0, st>>>(s);
+    linattn_step_kernel<T, 4, 4><<<grid(16), 256, 0, st>>>(s);
 }
 
 }  // namespace

@@ -237,6 +237,19 @@ def test_step(dtype, B, H, dk, dv):
 
 
 @gpu
+@pytest.mark.parametrize("dtype", [F32, BF16])
+@pytest.mark.parametrize("B,H,dk,dv", [(90, 3, 40, 128), (170, 2, 256, 100), (600, 1, 3, 4), (128, 1, 16, 256)])
+def test_step_of_many_states(dtype, B, H, dk, dv):
+    p = Problem(dtype, B, 1, H, dk, dv)
+    a = p.args()
+    (o, S), (mo, mS) = O.linattn(*a, p.scale, None, np64(p.S0)), O.linattn(*a, p.scale, None, np64(p.S0), magnitude=True)
+    state, got = p.S0.cuda(), torch.full((B, H, dv), float("nan"), dtype=dtype, device="cuda")
+    mdh.mdh_linattn_step(p.q[:, 0].cuda(), p.k[:, 0].cuda(), p.v[:, 0].cuda(), p.g.cuda(), state, got, p.scale)
+    close(got, o[:, 0], mo[:, 0], dtype, dk + 32, "o")
+    close(state, S, mS, F32, 32, "state")
+
+
+@gpu
 def test_step_in_slots_and_strides():
     p = Problem(BF16, 4, 1, 3, 32, 48)
     q, k, v = (t[:, 0].cuda() for t in (p.q, p.k, p.v))
