@@ -4,8 +4,11 @@
 // or, with few of them, by one trip to it.  A workgroup owns W columns of one state, a lane 4 columns
 // of every 1024/W-th row: the sum over the rows that q asks for stays in the workgroup.  A lane's first eight loads are
 // under way before anything is waited for.  W is 64 where that gives the chip two workgroups a compute unit, else 16.
-// Measured in a graph, W = 128 / 64 / 16, states of 128 x 128: 32 of them 8.6 / 5.4 / 4.4 us, 128 12.4 / 8.2 / 7.9, 256
-// 14.8 / 10.8 / 12.9, 1024 33 / 32 / 40, 4096 117 / 112 / 164 (4.8 TB/s); of 64 x 64: 512 7.9 / 7.4 / 9.6.
+// Loads and stores leave the caches to others: between two tokens of one layer come all the other layers, whose states push
+// its own out (cached / not, the states cold: 32 of 128 x 128 4.4 / 4.0 us, 512 17.3 / 12.4, 1024 32.3 / 26.0, 4096 113.7 /
+// 102.4 = 5.2 TB/s; of one layer called again and again 3.8 / 3.8, 10.5 / 10.0, 24.8 / 22.8, 89.6 / 101.8).
+// Measured in a graph, W = 64 / 16, states of 128 x 128: 32 of them 5.3 / 4.0 us, 128 6.3 / 6.1, 256 7.9 / 11.8, 1024
+// 26.0 / 47.1; W = 128: 9.7, 10.8, 12.6, 25.4.
 #include "mdh_internal.h"
 #include "mdh_types.h"
 
@@ -45,7 +48,7 @@ __global__ __launch_bounds__(256) void linattn_step_kernel(StepArgs s) {
   auto read = [&](int r0) {
 #pragma unroll
     for (int u = 0; u < U; ++u)
-      if (col < s.dv && r0 + u * RP < s.dk) x[u] = *(const fv*)(st + (int64_t)(r0 + u * RP) * s.dv);
+      if (col < s.dv && r0 + u * RP < s.dk) x[u] = __builtin_nontemporal_load((const fv*)(st + (int64_t)(r0 + u * RP) * s.dv));
   };
   read(row);
   const T* pv = (const T*)s.v.p + b * s.v.sb + (h / s.v.group) * s.v.sh;
@@ -73,7 +76,7 @@ __global__ __launch_bounds__(256) void linattn_step_kernel(StepArgs s) {
         x[u][e] = l * x[u][e] + kr * v[e];
         sum[e] += qr * x[u][e];
       }
-      *(fv*)(st + (int64_t)r * s.dv) = x[u];
+      __builtin_nontemporal_store(x[u], (fv*)(st + (int64_t)r * s.dv));
     }
   }
   // rows: over the lanes of a wavefront that share columns, then over the wavefronts
