@@ -511,8 +511,7 @@ typedef enum mdh_dtype { MDH_F32 = 0, MDH_BF16 = 1 } mdh_dtype;
  *   q, k, v  (B, T, Hq, dk), (B, T, Hk, dk), (B, T, Hv, dv); o: (B, T, H, dv); of type dtype
  *   strides  12 numbers, (batch, token, head) of q, k, v, o in elements; channels are adjacent.
  *            NULL: all dense.  Inputs may have stride 0 (one value for all), and 64 tokens lie within 2^31
- *            bytes.  Any alignment that the
- *            type has; 16 bytes (base, strides and rows) are several times faster.
+ *            bytes.  Any alignment that the type has; 16 bytes (base, strides and rows) are faster.
  *   log_decay  H fp32, natural logarithm, <= 0; -infinity is l = 0
  *   lengths  B int32 or NULL (all T).  Tokens from lengths[b] on are not read (any value, NaN too);
  *            their outputs are 0.  Less than 0 counts as 0, more than T as T.

@@ -17,6 +17,11 @@
 // fp32 operands are three bf16 slices each (24 bits, cut off), and products the six largest of nine (2^-23 of a product is
 // lost).  bf16 operands are one slice; scores and S are rounded to one slice where they are operands (2^-9 of a
 // term, as the output's own rounding), but what is added to S is not: c_j times its decay is three slices.
+//
+// Bound by memory where the sequence is long: 65536 x 16 heads of 128 x 128, bf16, 130 us for the states of 32 segments (4.1
+// TB/s; 122 without its arithmetic), 15 for their prefix sum and 240-250 for the pass (4.4 TB/s, 280 TFLOP/s).  2048 x 32
+// heads: 15 + 8 + 28 us, the last for four runs of a workgroup one after the other.  Trained, 8 x 4096 x 16 heads: 71 + 11 +
+// 140 for the forward call, 440-470 for the three passes of the backward call, which read nine tensors and write three.
 #include "mdh_internal.h"
 #include "mdh_types.h"
 
