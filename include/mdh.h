@@ -507,7 +507,8 @@ typedef enum mdh_dtype { MDH_F32 = 0, MDH_BF16 = 1 } mdh_dtype;
  * parts before a part is a matrix instead of mdh_scan's one number.
  *   sizes    (B, T, H, Hq, Hk, Hv, dk, dv): H heads of decays, states and outputs; q, k and v have
  *            Hq, Hk and Hv heads, which divide H: head h reads theirs number h / (H / Hq), ...
- *            B, T >= 0, the others >= 1, dk and dv <= 256.
+ *            B, T >= 0, the others >= 1, dk and dv <= 256.  A call has fewer than 2^24 workgroups (MDH_ERR_SIZE),
+ *            one for each 128 or 64 columns of each of the B * H states, in the backward call of three passes.
  *   q, k, v  (B, T, Hq, dk), (B, T, Hk, dk), (B, T, Hv, dv); o: (B, T, H, dv); of type dtype
  *   strides  12 numbers, (batch, token, head) of q, k, v, o in elements; channels are adjacent.
  *            NULL: all dense.  Inputs may have stride 0 (one value for all), and 64 tokens lie within 2^31
@@ -564,6 +565,7 @@ mdh_status mdh_linattn_step(const int64_t* sizes, mdh_dtype dtype, const void* q
  *   z = (x - mean) * rstd * weight[c] + bias[c],  rstd = 1 / sqrt(variance + eps)
  *   y = act(z),  or  y = z * act(gate)  where there is a gate
  *   sizes    (N, S, C, G), G divides C.  S = 1: rows, as the heads of a token; S = H*W: mdh_mcc's images.
+ *            Fewer than 2^24 images, N * G and N * S below 2^31 (MDH_ERR_SIZE).
  *            N or S = 0 is an empty call (mean and rstd stay as they are; gradients of weight and bias are 0).
  *   x, gate, y  N*S rows of C elements of type dtype; row_strides: 3 numbers, elements from row to row
  *            of x, gate, y (NULL: dense); weight, bias: C fp32, or NULL (1 and 0)

@@ -764,7 +764,7 @@ mdh_status launch_group_norm(const GroupNormCall& c, hipStream_t st) {
   }
   Slabs s = slabs_of(c, V);
   const int64_t blocks = c.N * s.shares * s.slabs;
-  if (blocks > 0x7fffffff) return MDH_ERR_SIZE;
+  if (blocks >= 1 << 24) return MDH_ERR_SIZE;  // 2^32 lanes
   s.stats = c.ws;
   with_type(c, V, [&](auto T_, auto V_) {
     slabs_stats_kernel<decltype(T_), V_.value><<<dim3((unsigned)blocks), kLanes, 0, st>>>(c, s);
@@ -789,7 +789,7 @@ mdh_status launch_group_norm_backward(const GroupNormCall& c, hipStream_t st) {
   }
   Slabs s = slabs_of(c, V);
   const int64_t blocks = c.N * s.shares * s.slabs, more = cdiv(c.C, 32);
-  if (blocks + more > 0x7fffffff) return MDH_ERR_SIZE;
+  if (blocks + more >= 1 << 24) return MDH_ERR_SIZE;
   s.stats = c.ws;
   s.parts = (float*)((char*)c.ws + stats_bytes(c, s));
   s.last = (int)blocks;

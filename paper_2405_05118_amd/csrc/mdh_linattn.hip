@@ -656,18 +656,22 @@ __global__ __launch_bounds__(256) void linattn_segments_kernel(CombineArgs a) {
   }
 }
 
-// Gradients of shared heads: a workgroup for each token, a lane for the channels that are 256 apart.
+// Gradients of shared heads: a workgroup for each token (more tokens than a grid has: for some), a lane for the channels that
+// are 256 apart.
+constexpr int64_t kShareGrid = 1 << 20;
 template <typename T>
-__global__ __launch_bounds__(256) void linattn_share_kernel(const float* __restrict__ src, HeadView dst, int T_, int H, int heads, int d) {
-  const int64_t bt = blockIdx.x;
+__global__ __launch_bounds__(256) void linattn_share_kernel(const float* __restrict__ src, HeadView dst, int64_t tokens, int T_, int H,
+                                                            int heads, int d) {
   const int g = H / heads;
-  const float* from = src + bt * H * d;
-  T* to = (T*)dst.p + bt / T_ * dst.sb + bt % T_ * dst.st;
-  for (int e = threadIdx.x; e < heads * d; e += 256) {
-    const int hs = e / d, ch = e % d;
-    float sum = 0.f;
-    for (int j = 0; j < g; ++j) sum += from[(int64_t)(hs * g + j) * d + ch];
-    to[hs * dst.sh + ch] = from_float<T>(sum);
+  for (int64_t bt = blockIdx.x; bt < tokens; bt += kShareGrid) {
+    const float* from = src + bt * H * d;
+    T* to = (T*)dst.p + bt / T_ * dst.sb + bt % T_ * dst.st;
+    for (int e = threadIdx.x; e < heads * d; e += 256) {
+      const int hs = e / d, ch = e % d;
+      float sum = 0.f;
+      for (int j = 0; j < g; ++j) sum += from[(int64_t)(hs * g + j) * d + ch];
+      to[hs * dst.sh + ch] = from_float<T>(sum);
+    }
   }
 }
 
@@ -678,7 +682,7 @@ mdh_status run(const PassArgs& a, hipStream_t st) {
   int tiles = 0;
   for (int i = 0; i < a.n; ++i) tiles += a.tiles[i];
   const int64_t blocks = a.c.B * a.c.H * (STATE ? a.seg[0].n - 1 : a.seg[0].n) * tiles;
-  if (blocks > 0x7fffffff) return MDH_ERR_SIZE;
+  if (blocks >= 1 << 24) return MDH_ERR_SIZE;  // 2^32 lanes
   const void* kern = (const void*)linattn_runs_kernel<T, KP, NB, STATE, ACCESS>;
   const mdh_status r = allow_dynamic_lds(kern, X::kBytes, done);
   if (r != MDH_OK) return r;
@@ -833,12 +837,12 @@ mdh_status launch_linattn_share(const LinattnCall& c, const float* src, int d, c
                                 hipStream_t st) {
   const int64_t tokens = c.B * c.T;
   if (tokens == 0) return MDH_OK;
-  if (tokens > 0x7fffffff) return MDH_ERR_SIZE;
+  const dim3 grid((unsigned)(tokens < kShareGrid ? tokens : kShareGrid));
   clear_stale_error();
   if (dtype == MDH_BF16)
-    linattn_share_kernel<bf16><<<dim3((unsigned)tokens), 256, 0, st>>>(src, dst, (int)c.T, c.H, heads, d);
+    linattn_share_kernel<bf16><<<grid, 256, 0, st>>>(src, dst, tokens, (int)c.T, c.H, heads, d);
   else
-    linattn_share_kernel<float><<<dim3((unsigned)tokens), 256, 0, st>>>(src, dst, (int)c.T, c.H, heads, d);
+    linattn_share_kernel<float><<<grid, 256, 0, st>>>(src, dst, tokens, (int)c.T, c.H, heads, d);
   return launch_status();
 }
 

@@ -111,7 +111,7 @@ void step(const StepArgs& s, bool vec, hipStream_t st) {
 
 mdh_status launch_linattn_step(const LinattnCall& c, const HeadView& q, const HeadView& k, const HeadView& v,
                                const HeadView& o, int dk, int dv, float scale, float* state, int dtype, hipStream_t st) {
-  if (c.B * c.H > 0x7fffffff) return MDH_ERR_SIZE;
+  if (c.B * c.H >= 1 << 24) return MDH_ERR_SIZE;  // 2^32 lanes
   const StepArgs s{c, q, k, v, o, dk, dv, scale, state};
   const bool vec = dv % 4 == 0 && (uintptr_t)state % 16 == 0;
   clear_stale_error();

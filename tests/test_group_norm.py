@@ -258,6 +258,13 @@ def _raw(sizes, dtype=0, x=64, y=64, act=0, strides=None, ws=1 << 20, nws=1 << 4
     return mdh.lib().mdh_group_norm(mdh.binding._sizes(sizes), dtype, x, None, st, None, None, 1e-5, act, y, None, None, ws, nws, None)
 
 
+def test_more_images_than_a_launch_has_are_refused():
+    sizes = mdh.binding._sizes((1 << 24, 2, 16, 4))
+    assert mdh.lib().mdh_group_norm(sizes, 0, 64, None, None, None, None, 1e-5, 0, 64, None, None, 1 << 20, 1 << 60, None) == E_SIZE
+    assert mdh.lib().mdh_group_norm_backward(sizes, 0, 64, None, 64, None, None, None, 64, 64, 0, 64, None, None, None, 1 << 20, 1 << 60,
+                                             None) == E_SIZE
+
+
 def test_refusals():
     ok = (2, 5, 16, 4)
     for sizes in ((-1, 5, 16, 4), (2, -5, 16, 4), (2, 5, 0, 4), (2, 5, 16, 0), (2, 5, 16, 3), (1 << 20, 1 << 20, 16, 4)):

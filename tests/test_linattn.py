@@ -422,6 +422,13 @@ def test_refusals():
     assert step((1, 4, 4, 4, 4, 16, 16), state=None) == E_NULL and step((1, 4, 4, 4, 4, 16, 16), q=None) == E_NULL
 
 
+def test_more_lanes_than_a_launch_has_are_refused():
+    many = 1 << 24
+    assert _raw((many, 1, 1, 1, 1, 1, 16, 16)) == E_SIZE and _raw((many // 2, 1, 1, 1, 1, 1, 16, 256)) == E_SIZE
+    S = mdh.binding._sizes
+    assert mdh.lib().mdh_linattn_step(S((many // 2, 2, 2, 2, 2, 16, 16)), 0, 64, 64, 64, None, 64, 1.0, 64, None, 0, 64, None) == E_SIZE
+
+
 def test_binding_refuses_what_does_not_fit():
     x = torch.zeros(1, 4, 2, 8)
     g = torch.zeros(2)
