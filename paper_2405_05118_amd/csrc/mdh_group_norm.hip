@@ -12,10 +12,10 @@
 // Sums over shares are taken in a fixed order.  Gradients of weight and bias: one row of the workspace for each share, summed
 // by the workgroups of the second launch that come after those for the images (teams: a launch of their own).
 //
-// Measured, bf16 unless said (inputs not in the caches).  Teams: 16384 rows of 4096 in 32 groups with a gate 89 us (4.5 TB/s),
-// their gradients 139 + 7 (4.8 TB/s); one such row 3.2.  Slabs: 8 x 128 x 128 x 256 in 32 groups, silu, 15 + 37 us (67 MB read,
+// Measured, bf16 unless said (inputs not in the caches).  Teams: 16384 rows of 4096 in 32 groups with a gate 81 us (5.0 TB/s),
+// their gradients 152 + 5 (4.4 TB/s; with 1024 workgroups 139 + 7); one such row 3.2.  Slabs: 8 x 128 x 128 x 256 in 32 groups, silu, 15 + 37 us (67 MB read,
 // read again and written: 3.9 TB/s), gradients 46 + 57; fp32 16 x 56 x 56 x 64 in 32 groups 7 + 11.  Stores that leave the
-// caches alone are up to a tenth faster (16384 rows, trained: 227 us for 238) and cost whoever reads the output next as much
+// caches alone are up to a tenth faster (16384 rows, trained: 5 %) and cost whoever reads the output next as much
 // (2048 rows and a sum after it: 20.1 us for 19.5): not taken.
 #include "mdh_act.h"
 #include "mdh_internal.h"
@@ -645,8 +645,6 @@ int pieces(const GroupNormCall& c, int V) {
   return P <= 64 ? 1 : P <= 128 ? 2 : 4;
 }
 
-constexpr int kTeamShares = 1024;
-
 Teams teams_of(const GroupNormCall& c, int V, bool backward) {
   Teams t{};
   const int P = c.C / c.G / V, NP = pieces(c, V);
@@ -655,8 +653,12 @@ Teams teams_of(const GroupNormCall& c, int V, bool backward) {
   const int most = kLanes / t.L;
   t.across = c.G < most ? c.G : most;
   const int64_t slabs = cdiv(c.G, t.across), step = kLanes / (t.L * t.across);
-  // 2048 workgroups fill the chip eight deep; in the backward call each leaves a row of the workspace
-  int64_t shares = (backward ? kTeamShares : 2048) / slabs;
+  // Workgroups.  Forward: four goes each, within 1024 to 8192 (16384 rows of 4096 with a gate: 8192 79-81 us, 2048 88-90, 16384 86;
+  // 2048 rows: 1024 12.9 us, 2048 13.9, 8192 14.7).  In the backward call each leaves a row of the workspace, which a launch
+  // adds up: two a compute unit (gradients and forward, 4096 rows of 2048: 512 47 us, 1024 55, 256 51; 16384 rows of 4096 236,
+  // 239, 303).
+  const int64_t goes = slabs * cdiv(c.N, step), most_wg = goes / 4 < 1024 ? 1024 : goes / 4 > 8192 ? 8192 : goes / 4;
+  int64_t shares = (backward ? 512 : most_wg) / slabs;
   if (shares < 1) shares = 1;
   if (shares > cdiv(c.N, step)) shares = cdiv(c.N, step);
   t.rows = (int)(cdiv(cdiv(c.N, shares), step) * step);
