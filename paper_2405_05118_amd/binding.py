@@ -562,6 +562,8 @@ def mdh_group_norm(x, weight, bias, y, groups: int, eps: float = 1e-5, act: int 
     weight, bias: (C,) float32 or None; mean, rstd: (N, groups) float32 or None, what the backward call wants."""
     L = _lib or lib()
     shape = x.shape
+    if len(shape) < 2:
+        raise ValueError("x has shape %s: rows of channels are required, one row too is (1, C)" % (tuple(shape),))
     N, C = shape[0], shape[-1]
     dt = x.dtype
     d = _dtype_of(dt)
@@ -580,6 +582,8 @@ def mdh_group_norm_backward(x, weight, bias, mean, rstd, d_y, d_x, d_weight, d_b
     """Gradients of mdh_group_norm, whose mean and rstd it takes; d_weight, d_bias: (C,) float32 or None."""
     L = _lib or lib()
     shape = x.shape
+    if len(shape) < 2:
+        raise ValueError("x has shape %s: rows of channels are required, one row too is (1, C)" % (tuple(shape),))
     N, C = shape[0], shape[-1]
     dt = x.dtype
     d = _dtype_of(dt)

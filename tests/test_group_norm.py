@@ -287,3 +287,14 @@ def test_refusals():
         mdh.mdh_group_norm(x, None, None, x, 4)
     with pytest.raises(ValueError):
         mdh.mdh_group_norm_backward(x, None, None, None, None, x, x, None, None, 4, gate=x)
+
+
+def test_binding_refuses_fewer_than_two_dimensions():
+    """(C,) would be C rows of C channels.  Refused before a pointer is asked for: these tensors are not on the GPU either."""
+    for x in (torch.zeros(64), torch.zeros(())):
+        with pytest.raises(ValueError):
+            mdh.mdh_group_norm(x, None, None, x, 4)
+        with pytest.raises(ValueError):
+            mdh.mdh_group_norm(x, None, None, x, 4, gate=x)
+        with pytest.raises(ValueError):
+            mdh.mdh_group_norm_backward(x, None, None, x, x, x, x, None, None, 4)
