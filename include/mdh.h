@@ -572,6 +572,8 @@ mdh_status mdh_linattn_step(const int64_t* sizes, mdh_dtype dtype, const void* q
  *   mean, rstd  N*G fp32 each, or NULL: what the backward call wants
  * Variances are sums of squared differences from a mean (no squares of x are subtracted), in fp32.
  * Inf or NaN in a group makes that group NaN and no other.  One value a group (variance 0) gives bias.
+ * relu of -infinity (a masked channel's gate or bias) is 0, and its slope; silu and gelu follow their formulas, which
+ * have no value there (-infinity times 0).
  */
 enum { MDH_ACT_NONE = 0, MDH_ACT_RELU = 1, MDH_ACT_SILU = 2, MDH_ACT_GELU = 3 /* z Phi(z) */ };
 size_t mdh_group_norm_workspace_size(const int64_t* sizes, mdh_dtype dtype, int32_t backward);

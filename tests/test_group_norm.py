@@ -298,3 +298,25 @@ def test_binding_refuses_fewer_than_two_dimensions():
             mdh.mdh_group_norm(x, None, None, x, 4, gate=x)
         with pytest.raises(ValueError):
             mdh.mdh_group_norm_backward(x, None, None, x, x, x, x, None, None, 4)
+
+
+@gpu
+@pytest.mark.parametrize("dtype", [F32, BF16])
+@pytest.mark.parametrize("N,S,C,G", [(5, 1, 128, 4), (2, 77, 48, 6), (1, 6000, 16, 4), (2, 1, 20000, 1)])
+def test_relu_of_minus_infinity(dtype, N, S, C, G):
+    """Channels whose gate or bias is -infinity: relu and its slope are 0 there, as for any other negative number."""
+    p = Problem(dtype, N, S, C, G, "relu", gate=True)
+    off = torch.arange(C) % 3 == 1
+    p.gate[..., off] = -1.0
+    p.check()
+    want = p.run()
+    p.gate[..., off] = -float("inf")
+    got = p.run()
+    assert all(torch.equal(a, b) for a, b in zip(got, want))
+    ref = O.group_norm(np64(p.x), np64(p.w), np64(p.b), G, p.eps, "relu", np64(p.gate))[0]
+    assert not ref[..., off.numpy()].any() and not got[0][..., off.cuda()].any()
+    p = Problem(dtype, N, S, C, G, "relu")
+    p.b[off] = -1e30
+    want = p.run()
+    p.b[off] = -float("inf")
+    assert all(torch.equal(a, b) for a, b in zip(p.run()[:6], want[:6]))
