@@ -378,12 +378,13 @@ __device__ __forceinline__ SlabLane place(const GroupNormCall& c, const Slabs& s
 struct alignas(16) Stat {
   float n, mean, m2, none;
 };
-// of two parts
+// Of two parts.  An empty one is passed over: merged, its mean of 0 would move the other's by the rounding of 1/n, and from
+// 2^64 on square to infinity.
 __device__ __forceinline__ Stat operator+(const Stat& a, const Stat& b) {
-  const float n = a.n + b.n;
-  if (n == 0.f) return a;
-  const float d = b.mean - a.mean, f = b.n * __builtin_amdgcn_rcpf(n);
-  return Stat{n, a.mean + d * f, a.m2 + b.m2 + d * d * a.n * f, 0.f};
+  if (b.n == 0.f) return a;
+  if (a.n == 0.f) return b;
+  const float n = a.n + b.n, d = b.mean - a.mean, f = b.n * __builtin_amdgcn_rcpf(n), df = d * f;
+  return Stat{n, a.mean + df, a.m2 + b.m2 + df * d * a.n, 0.f};
 }
 
 // Combines val over the lanes of each group of a slab: positions first, then the group's pieces; the result is in the lane with

@@ -320,3 +320,29 @@ def test_relu_of_minus_infinity(dtype, N, S, C, G):
     want = p.run()
     p.b[off] = -float("inf")
     assert all(torch.equal(a, b) for a, b in zip(p.run()[:6], want[:6]))
+
+
+# (counts of a share, such as 82 and 110, whose product with their reciprocal need not be 1)
+PARTS = [(16, 1312, 64, 32), (16, 1760, 64, 32), (2, 77, 48, 6), (1, 6000, 16, 4), (3, 1, 128, 4), (2, 1, 20000, 1)]
+
+
+@gpu
+@pytest.mark.parametrize("dtype", [F32, BF16])
+@pytest.mark.parametrize("N,S,C,G", PARTS)
+def test_one_value_a_group_in_any_number_of_parts(dtype, N, S, C, G):
+    p = Problem(dtype, N, S, C, G, "none")
+    p.x = torch.full((N, S, C), 3.0, dtype=dtype)
+    y, mean, rstd, dx, dw, _, _ = p.run()
+    assert torch.equal(y.cpu(), p.b.to(dtype).expand(N, S, C)) and (mean == 3).all()
+    assert torch.allclose(rstd, torch.full_like(rstd, p.eps ** -0.5), rtol=1e-6)
+    assert torch.isfinite(dx.float()).all() and not dw.any()
+
+
+@gpu
+@pytest.mark.parametrize("N,S,C,G", PARTS)
+def test_means_whose_square_is_no_float(N, S, C, G):
+    """Values around 1e20 (bf16: 2.5e19, in steps of 1.4e17): differences from their mean square to 1e34, they themselves to infinity."""
+    for dtype, mean in ((F32, 1e20), (BF16, 2.5e19)):
+        p = Problem(dtype, N, S, C, G, "none")
+        p.x = (mean + 1e17 * rand(3, N, S, C)).to(dtype)
+        p.check()
