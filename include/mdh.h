@@ -571,7 +571,8 @@ mdh_status mdh_linattn_step(const int64_t* sizes, mdh_dtype dtype, const void* q
  *            of x, gate, y (NULL: dense); weight, bias: C fp32, or NULL (1 and 0)
  *   mean, rstd  N*G fp32 each, or NULL: what the backward call wants
  * Variances are sums of squared differences from a mean (no squares of x are subtracted), in fp32.
- * Inf or NaN in a group makes that group NaN and no other.  One value a group (variance 0) gives bias.
+ * Inf or NaN in a group makes that group NaN and no other.  One value a group (variance 0) gives bias, whatever
+ * the value is (while the sum of the group's is a float).
  * relu of -infinity (a masked channel's gate or bias) is 0, and its slope; silu and gelu follow their formulas, which
  * have no value there (-infinity times 0).
  */

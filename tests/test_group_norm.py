@@ -346,3 +346,21 @@ def test_means_whose_square_is_no_float(N, S, C, G):
         p = Problem(dtype, N, S, C, G, "none")
         p.x = (mean + 1e17 * rand(3, N, S, C)).to(dtype)
         p.check()
+
+
+@gpu
+@pytest.mark.parametrize("dtype", [F32, BF16])
+@pytest.mark.parametrize("N,S,C,G", PARTS + [(3, 1, 24, 8), (70, 1, 512, 4), (2, 1021, 35, 5), (2, 3000, 8, 8), (1, 700, 1028, 4)])
+def test_one_value_a_group_whatever_it_is(dtype, N, S, C, G):
+    """Another constant for every group, most of whose sums are rounded: the mean is the value, the output the bias."""
+    p = Problem(dtype, N, S, C, G, "none")
+    values = torch.tensor([1000.3, 0.1, -12345.678, 1e-3, 7.7e8, -3.3e20, 1 / 3, 1e-20, 65537.0, -1.1])
+    at = torch.arange(N * G).reshape(N, G) % len(values)
+    group = values[at].to(dtype)
+    p.x = group.repeat_interleave(C // G, 1)[:, None, :].expand(N, S, C).contiguous()
+    y, mean, rstd, dx, dw, _, _ = p.run()
+    assert torch.equal(mean.cpu(), group.float())
+    assert torch.equal(y.cpu(), p.b.to(dtype).expand(N, S, C))
+    moderate = (values[at].abs() <= 2000).cuda()
+    assert torch.allclose(rstd[moderate], torch.full_like(rstd[moderate], p.eps ** -0.5), rtol=1e-6)
+    assert torch.isfinite(rstd).all() and torch.isfinite(dx.float()).all() and not dw.any()
