@@ -366,7 +366,8 @@ struct SlabLane {
   int across, down;                  // lanes along the channels and along the positions
   int c, r;                          // this one's; r >= down: idle
   int g, ch;                         // its group and first channel
-  int s0, s1;                        // positions
+  int64_t row0;                      // the share's first row
+  int rows;                          // and its positions
 };
 template <int V>
 __device__ __forceinline__ SlabLane place(const GroupNormCall& c, const Slabs& s, int block) {
@@ -386,8 +387,9 @@ __device__ __forceinline__ SlabLane place(const GroupNormCall& c, const Slabs& s
   p.r = threadIdx.x / p.across;
   p.g = p.g0 + (s.per_group > 1 ? 0 : p.c / P);
   p.ch = p.g0 * D + (begin + p.c) * V;
-  p.s0 = p.share * s.rows;
-  p.s1 = min((int)c.S, p.s0 + s.rows);
+  const int64_t s0 = (int64_t)p.share * s.rows;
+  p.row0 = p.n * c.S + s0;
+  p.rows = (int)min(c.S - s0, (int64_t)s.rows);
   return p;
 }
 
@@ -437,14 +439,13 @@ __global__ __launch_bounds__(kLanes) void slabs_stats_kernel(GroupNormCall c, Sl
   const SlabLane p = place<V>(c, s, blockIdx.x);
   const int P = c.C / c.G / V;
   Stat mine{0.f, 0.f, 0.f, 0.f};
-  const int64_t row0 = p.n * c.S;
   if (p.r < p.down)
-    for (int r0 = p.s0 + p.r; r0 < p.s1; r0 += kBatch * p.down) {
+    for (int r0 = p.r; r0 < p.rows; r0 += kBatch * p.down) {
       float x[kBatch][V];
-      const int n = min(kBatch, (p.s1 - r0 + p.down - 1) / p.down);
+      const int n = min(kBatch, (p.rows - r0 + p.down - 1) / p.down);
 #pragma unroll
       for (int u = 0; u < kBatch; ++u)
-        if (u < n) load<T, V>(at<const T>(c.x, row0 + r0 + u * p.down, p.ch), x[u]);
+        if (u < n) load<T, V>(at<const T>(c.x, p.row0 + r0 + u * p.down, p.ch), x[u]);
       float sum = 0.f, off = 0.f, q = 0.f;
 #pragma unroll
       for (int u = 0; u < kBatch; ++u)
@@ -501,17 +502,16 @@ template <typename T, int V>
 __global__ __launch_bounds__(kLanes) void slabs_forward_kernel(GroupNormCall c, Slabs s) {
   __shared__ Stat lds[kLanes];
   const SlabLane p = place<V>(c, s, blockIdx.x);
-  const int64_t row0 = p.n * c.S;
   Raw<T, V> x_raw[kBatch], gate[kBatch];
   auto read = [&](int r0) {
 #pragma unroll
     for (int u = 0; u < kBatch; ++u)
-      if (r0 + u * p.down < p.s1) {
-        x_raw[u] = *(const Raw<T, V>*)at<T>(c.x, row0 + r0 + u * p.down, p.ch);
-        if (c.gate.p) gate[u] = *(const Raw<T, V>*)at<T>(c.gate, row0 + r0 + u * p.down, p.ch);
+      if (r0 + u * p.down < p.rows) {
+        x_raw[u] = *(const Raw<T, V>*)at<T>(c.x, p.row0 + r0 + u * p.down, p.ch);
+        if (c.gate.p) gate[u] = *(const Raw<T, V>*)at<T>(c.gate, p.row0 + r0 + u * p.down, p.ch);
       }
   };
-  if (p.r < p.down) read(p.s0 + p.r);  // (on its way while the statistics are combined)
+  if (p.r < p.down) read(p.r);  // (on its way while the statistics are combined)
   combine_shares(c, s, p, Stat{0.f, 0.f, 0.f, 0.f}, lds, [](const Stat& a, const Stat& b) { return a + b; });
   const Stat st = lds[p.g - p.g0];
   const float mean = st.mean, rstd = 1.f / sqrtf(st.m2 / st.n + c.eps);
@@ -524,14 +524,14 @@ __global__ __launch_bounds__(kLanes) void slabs_forward_kernel(GroupNormCall c, 
   float w[V], b[V];
   params<V>(c.weight, p.ch, 1.f, w);
   params<V>(c.bias, p.ch, 0.f, b);
-  for (int r0 = p.s0 + p.r; r0 < p.s1; r0 += kBatch * p.down) {
-    if (r0 != p.s0 + p.r) read(r0);
+  for (int r0 = p.r; r0 < p.rows; r0 += kBatch * p.down) {
+    if (r0 != p.r) read(r0);
 #pragma unroll
     for (int u = 0; u < kBatch; ++u)
-      if (r0 + u * p.down < p.s1) {
+      if (r0 + u * p.down < p.rows) {
         float x[V];
         expand<T, V>(x_raw[u], x);
-        result<T, V>(c, row0 + r0 + u * p.down, p.ch, x, gate[u], mean, rstd, w, b);
+        result<T, V>(c, p.row0 + r0 + u * p.down, p.ch, x, gate[u], mean, rstd, w, b);
       }
   }
 }
@@ -570,15 +570,14 @@ __global__ __launch_bounds__(kLanes) void slabs_backward_kernel(GroupNormCall c,
   params<V>(c.bias, p.ch, 0.f, b);
 #pragma unroll
   for (int i = 0; i < V; ++i) dw[i] = db[i] = 0.f;
-  const int64_t row0 = p.n * c.S;
   if (p.r < p.down)
-    for (int r0 = p.s0 + p.r; r0 < p.s1; r0 += kBatchBack * p.down) {
+    for (int r0 = p.r; r0 < p.rows; r0 += kBatchBack * p.down) {
       Raw<T, V> x_raw[kBatchBack], dy_raw[kBatchBack], gate_raw[kBatchBack];
-      const int n = min(kBatchBack, (p.s1 - r0 + p.down - 1) / p.down);
+      const int n = min(kBatchBack, (p.rows - r0 + p.down - 1) / p.down);
 #pragma unroll
       for (int k = 0; k < kBatchBack; ++k)
         if (k < n) {
-          const int64_t row = row0 + r0 + k * p.down;
+          const int64_t row = p.row0 + r0 + k * p.down;
           x_raw[k] = *(const Raw<T, V>*)at<T>(c.x, row, p.ch);
           dy_raw[k] = *(const Raw<T, V>*)at<T>(c.y, row, p.ch);
           if (c.gate.p) gate_raw[k] = *(const Raw<T, V>*)at<T>(c.gate, row, p.ch);
@@ -586,7 +585,7 @@ __global__ __launch_bounds__(kLanes) void slabs_backward_kernel(GroupNormCall c,
 #pragma unroll
       for (int k = 0; k < kBatchBack; ++k)
         if (k < n) {
-          const int64_t row = row0 + r0 + k * p.down;
+          const int64_t row = p.row0 + r0 + k * p.down;
           float x[V], dy[V], gate[V] = {}, dz[V];
           expand<T, V>(x_raw[k], x);
           expand<T, V>(dy_raw[k], dy);
@@ -717,6 +716,7 @@ Slabs slabs_of(const GroupNormCall& c, int V) {
   const int at_once = 16 * (kLanes / s.groups) / s.per_group;
   if (shares > at_once) shares = at_once;
   if (shares < 1) shares = 1;
+  if (shares == 1 && c.S > 1 << 30) shares = 2;  // (a share's positions, and kBatch * kLanes more, are counted in 32 bits)
   s.rows = (int)cdiv(c.S, shares);
   s.shares = (int)cdiv(c.S, s.rows);
   return s;

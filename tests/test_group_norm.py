@@ -364,3 +364,29 @@ def test_one_value_a_group_whatever_it_is(dtype, N, S, C, G):
     moderate = (values[at].abs() <= 2000).cuda()
     assert torch.allclose(rstd[moderate], torch.full_like(rstd[moderate], p.eps ** -0.5), rtol=1e-6)
     assert torch.isfinite(rstd).all() and torch.isfinite(dx.float()).all() and not dw.any()
+
+
+@gpu
+def test_an_image_of_as_many_positions_as_are_taken():
+    """2^31 - 1 positions of one channel, all of what is in them at the end: no position's number, nor what is added to it, may wrap.
+    Sums of m values: relative errors of (24 + 4 sqrt(m / 256)) u = 7e-4 of the mean and the variance, two of them and a rounding
+    of 2^-8 in the outputs."""
+    m, tail = 2 ** 31 - 1, 1000
+    x, d_y = torch.zeros(1, m, 1, dtype=BF16, device="cuda"), torch.zeros(1, m, 1, dtype=BF16, device="cuda")
+    x[:, -tail:], d_y[:, -tail // 2:] = 1024.0, 1.0
+    y, dx = torch.full_like(x, float("nan")), torch.full_like(x, float("nan"))
+    mean, rstd, dw, db = (torch.full((1, 1) if i < 2 else (1,), float("nan"), device="cuda") for i in range(4))
+    ws = torch.empty(mdh.mdh_group_norm_workspace_size((1, m, 1, 1), BF16, True), dtype=torch.uint8, device="cuda")
+    mdh.mdh_group_norm(x, None, None, y, 1, 1e-5, mean=mean, rstd=rstd, workspace=ws)
+    mdh.mdh_group_norm_backward(x, None, None, mean, rstd, d_y, dx, dw, db, 1, workspace=ws)
+    rmean = tail * 1024 / m
+    rrstd = (tail * 1024 ** 2 / m - rmean ** 2 + 1e-5) ** -0.5
+    low, high = -rmean * rrstd, (1024 - rmean) * rrstd
+    t1, t2 = tail / 2 / m, tail / 2 * high / m
+    near = lambda got, want, limit: abs(float(got) - want) <= limit * abs(want)  # noqa: E731
+    assert near(mean, rmean, 1e-3) and near(rstd, rrstd, 1e-3) and near(dw, tail / 2 * high, 2e-3) and float(db) == tail / 2
+    assert near(y[0, 0, 0], low, 2e-3 + 2 ** -8) and near(y[0, -1, 0], high, 2e-3 + 2 ** -8)
+    for t in (y[0, :-tail, 0], y[0, -tail:, 0], dx[0, :-tail, 0], dx[0, -tail:-tail // 2, 0], dx[0, -tail // 2:, 0]):
+        assert bool((t == t[0]).all())
+    # (t - t1 - xh t2: about half of the first term is left)
+    assert near(dx[0, -1, 0], rrstd * (1 - t1 - high * t2), 8e-3 + 2 ** -8) and near(dx[0, -tail, 0], rrstd * (-t1 - high * t2), 8e-3 + 2 ** -8)
