@@ -536,7 +536,8 @@ mdh_status mdh_linattn(const int64_t* sizes, mdh_dtype dtype, const void* q, con
  * Gradients of mdh_linattn.  With E_T = d_final_state and G_t = E_t + scale q_t do_t^T, E_{t-1} = l G_t:
  *   dq_t = scale S_t do_t,   dk_t = G_t v_t,   dv_t = G_t^T k_t,   d_initial_state = E_0
  * -- the forward pass over other operands, for dk and dv from the last token to the first.  Those of
- * shared heads are summed in fp32 in a fixed order, and rounded once.
+ * shared heads are summed in fp32 in a fixed order, and rounded once; 64 tokens of all H heads in fp32 lie within 2^31
+ * bytes for that (MDH_ERR_SIZE): H * dk (q or k shared) and H * dv (v shared) are below 2^23 - 15.
  *   strides  21 numbers: (batch, token, head) of q, k, v, d_o, d_q, d_k, d_v; NULL: all dense
  *   initial_state  what the forward call had; d_final_state, d_initial_state: NULL = zeros / not wanted; two buffers
  *   workspace  mdh_linattn_workspace_size(sizes, dtype, 1) bytes, which hold what the forward call wants too

@@ -174,6 +174,7 @@ mdh_status mdh_linattn_backward(const int64_t* sizes, mdh_dtype dtype, const voi
     if (heads[i] == z.H) continue;
     p[i].out = view_of(ws, nullptr, z, z.H, p[i].dc, sizeof(float));
     p[i].out_f32 = 1;
+    if (out_of_reach(p[i].out, sizeof(float))) return MDH_ERR_SIZE;
     ws += share_bytes(z, heads[i], p[i].dc);
   }
   int64_t len;

@@ -442,3 +442,13 @@ def test_binding_refuses_what_does_not_fit():
         mdh.mdh_linattn_step(x[:, 0], x[:, 0, :, :4], x[:, 0], g, torch.zeros(1, 2, 8, 8), x[:, 0])
     with pytest.raises(TypeError):
         mdh.mdh_linattn_workspace_size((1, 4, 2, 2, 2, 2, 8, 8), torch.float64)
+
+
+@pytest.mark.parametrize("sizes", [(1, 64, 40000, 1, 40000, 40000, 256, 8), (1, 2, 40000, 40000, 1, 40000, 256, 8), (1, 64, 40000, 40000, 40000, 2, 8, 256)])
+@pytest.mark.parametrize("dtype", [0, 1])
+def test_shared_heads_whose_sums_are_out_of_reach_are_refused(sizes, dtype):
+    """64 tokens of the fp32 gradients of all heads take more than 2^31 bytes, though no operand does."""
+    S = mdh.binding._sizes
+    strides = S([x for heads, d in zip((*sizes[3:6], sizes[2], *sizes[3:6]), (8, 8, 8, 8, 256, 256, 256)) for x in (1 << 24, 1 << 17, d if heads > 1 else 0)])
+    assert mdh.lib().mdh_linattn_backward(S(sizes), dtype, 64, 64, 64, 64, strides, 64, 1.0, None, None, None, 64, 64, 64, None, 1 << 20, 1 << 60,
+                                          None) == E_SIZE
