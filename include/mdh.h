@@ -566,7 +566,9 @@ mdh_status mdh_linattn_step(const int64_t* sizes, mdh_dtype dtype, const void* q
  *   z = (x - mean) * rstd * weight[c] + bias[c],  rstd = 1 / sqrt(variance + eps)
  *   y = act(z),  or  y = z * act(gate)  where there is a gate
  *   sizes    (N, S, C, G), G divides C.  S = 1: rows, as the heads of a token; S = H*W: mdh_mcc's images.
- *            Fewer than 2^24 images, N * G and N * S below 2^31 (MDH_ERR_SIZE).
+ *            N * G and N * S below 2^31.  A call on images, or on rows of groups wider than 256 accesses (of 16 bytes
+ *            at most), has fewer than 2^24 workgroups, one or more for each n; a backward call has fewer than 2^29
+ *            channels (MDH_ERR_SIZE).
  *            N or S = 0 is an empty call (mean and rstd stay as they are; gradients of weight and bias are 0).
  *   x, gate, y  N*S rows of C elements of type dtype; row_strides: 3 numbers, elements from row to row
  *            of x, gate, y (NULL: dense); weight, bias: C fp32, or NULL (1 and 0)

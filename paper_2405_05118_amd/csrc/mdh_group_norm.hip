@@ -804,6 +804,8 @@ mdh_status launch_group_norm(const GroupNormCall& c, hipStream_t st) {
 }
 
 mdh_status launch_group_norm_backward(const GroupNormCall& c, hipStream_t st) {
+  const int64_t more = cdiv(c.C, 32);      // workgroups that add up parts
+  if (more >= 1 << 24) return MDH_ERR_SIZE;  // 2^32 lanes
   clear_stale_error();
   if (c.N == 0 || c.S == 0) return add_up(c, nullptr, 0, st);
   const int V = width(c, true);
@@ -818,7 +820,7 @@ mdh_status launch_group_norm_backward(const GroupNormCall& c, hipStream_t st) {
     return r != MDH_OK ? r : add_up(c, t.parts, t.shares, st);
   }
   Slabs s = slabs_of(c, V);
-  const int64_t blocks = c.N * s.shares * s.slabs, more = cdiv(c.C, 32);
+  const int64_t blocks = c.N * s.shares * s.slabs;
   if (blocks + more >= 1 << 24) return MDH_ERR_SIZE;
   s.stats = c.ws;
   s.parts = (float*)((char*)c.ws + stats_bytes(c, s));

@@ -390,3 +390,10 @@ def test_an_image_of_as_many_positions_as_are_taken():
         assert bool((t == t[0]).all())
     # (t - t1 - xh t2: about half of the first term is left)
     assert near(dx[0, -1, 0], rrstd * (1 - t1 - high * t2), 8e-3 + 2 ** -8) and near(dx[0, -tail, 0], rrstd * (-t1 - high * t2), 8e-3 + 2 ** -8)
+
+
+@pytest.mark.parametrize("sizes", [(1, 1, 1 << 29, 1 << 21), (3, 1, 1 << 30, 1 << 30), (0, 1, 1 << 29, 1), (1, 1, 1 << 29, 1)])
+def test_more_channels_than_a_launch_adds_up_are_refused(sizes):
+    """Gradients of weight and bias take a workgroup for 32 channels: fewer than 2^29, whatever the channels' groups are."""
+    assert mdh.lib().mdh_group_norm_backward(mdh.binding._sizes(sizes), 0, 64, None, 64, None, None, None, 64, 64, 0, 64, None, 64, 64, 1 << 20,
+                                             1 << 60, None) == E_SIZE
