@@ -397,3 +397,16 @@ def test_more_channels_than_a_launch_adds_up_are_refused(sizes):
     """Gradients of weight and bias take a workgroup for 32 channels: fewer than 2^29, whatever the channels' groups are."""
     assert mdh.lib().mdh_group_norm_backward(mdh.binding._sizes(sizes), 0, 64, None, 64, None, None, None, 64, 64, 0, 64, None, 64, 64, 1 << 20,
                                              1 << 60, None) == E_SIZE
+
+
+def test_a_workspace_that_is_missing_or_small_is_refused():
+    for sizes in ((1, 100000, 64, 4), (2, 1, 20000, 1)):
+        need = mdh.mdh_group_norm_workspace_size(sizes, F32, False)
+        assert need > 0
+        assert _raw(sizes, ws=None) == E_WS and _raw(sizes, nws=need - 1) == E_WS and _raw(sizes, ws=(1 << 20) + 8) == E_WS
+    for sizes in ((1, 100000, 64, 4), (2, 1, 20000, 1), (5, 1, 64, 4)):
+        need = mdh.mdh_group_norm_workspace_size(sizes, F32, True)
+        assert need > 0
+        for ws, n in ((None, 0), (1 << 20, need - 1), ((1 << 20) + 8, need)):
+            assert mdh.lib().mdh_group_norm_backward(mdh.binding._sizes(sizes), 0, 64, None, 64, None, None, None, 64, 64, 0, 64, None, None, None,
+                                                     ws, n, None) == E_WS

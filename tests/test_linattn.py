@@ -452,3 +452,30 @@ def test_shared_heads_whose_sums_are_out_of_reach_are_refused(sizes, dtype):
     strides = S([x for heads, d in zip((*sizes[3:6], sizes[2], *sizes[3:6]), (8, 8, 8, 8, 256, 256, 256)) for x in (1 << 24, 1 << 17, d if heads > 1 else 0)])
     assert mdh.lib().mdh_linattn_backward(S(sizes), dtype, 64, 64, 64, 64, strides, 64, 1.0, None, None, None, 64, 64, 64, None, 1 << 20, 1 << 60,
                                           None) == E_SIZE
+
+
+# rows of less than 16 bytes on either side of the state, which are read element by element (heads of 5 and 7: in bf16 only)
+NARROW = [(2, 130, 2, 3, 3, [130, 65]), (1, 70, 1, 3, 256, None), (1, 70, 1, 200, 5, [67]), (1, 2500, 1, 3, 5, None),
+          (3, 1500, 1, 5, 2, [1500, 0, 999]), (2, 100, 3, 100, 3, [33, 100]), (1, 129, 2, 1, 140, None), (2, 66, 1, 256, 1, [64, 66]),
+          (1, 700, 2, 7, 70, [650])]
+
+
+@gpu
+@pytest.mark.parametrize("dtype", [F32, BF16])
+@pytest.mark.parametrize("B,T,H,dk,dv,lengths", NARROW)
+def test_narrow_heads(dtype, B, T, H, dk, dv, lengths):
+    p = Problem(dtype, B, T, H, dk, dv, lengths=lengths, seed=T)
+    for b, n in enumerate(lengths or []):
+        for t in (p.q, p.k, p.v, p.d_o):
+            t[b, n:] = float("nan")
+    p.check()
+
+
+@gpu
+@pytest.mark.parametrize("dtype", [F32, BF16])
+@pytest.mark.parametrize("B,T,Hq,Hk,Hv,dk,dv", [(2, 1600, 2, 2, 6, 48, 40), (1, 1500, 6, 1, 2, 64, 24), (2, 1700, 1, 3, 1, 5, 6)])
+def test_shared_heads_in_segments(dtype, B, T, Hq, Hk, Hv, dk, dv):
+    """Sums over shared heads of gradients that several workgroups have made, one after another along the tokens."""
+    p = Problem(dtype, B, T, 6, dk, dv, Hq, Hk, Hv, lengths=[T - 90, T][:B])
+    assert mdh.mdh_linattn_workspace_size(p.sizes, dtype, False) > 0  # the states between segments
+    p.check()
