@@ -236,7 +236,7 @@ mdh_status group_norm_sizes(const int64_t* sizes, mdh_dtype dtype, int32_t act, 
   return MDH_OK;
 }
 RowView rows_of(const void* p, const int64_t* strides, int i, const GroupNormCall& c) {
-  RowView v{p, strides ? strides[i] : (int64_t)c.C, 0};
+  RowView v{p, strides ? strides[i] : (int64_t)c.C};
   if (c.N * c.S == 1) v.stride = 0;
   return v;
 }

@@ -333,11 +333,10 @@ mdh_status launch_linattn_step(const LinattnCall& c, const HeadView& q, const He
 
 // ---- group norm, channels last (mdh_group_norm.hip) ----
 
-// Row r of C elements is at p + r * stride (elements); vec: 16-byte accesses
+// Row r of C elements is at p + r * stride (elements)
 struct RowView {
   const void* p;
   int64_t stride;
-  int vec;
 };
 struct GroupNormCall {
   int64_t N, S;
