@@ -507,8 +507,8 @@ typedef enum mdh_dtype { MDH_F32 = 0, MDH_BF16 = 1 } mdh_dtype;
  * parts before a part is a matrix instead of mdh_scan's one number.
  *   sizes    (B, T, H, Hq, Hk, Hv, dk, dv): H heads of decays, states and outputs; q, k and v have
  *            Hq, Hk and Hv heads, which divide H: head h reads theirs number h / (H / Hq), ...
- *            B, T >= 0, the others >= 1, dk and dv <= 256.  A call has fewer than 2^24 workgroups (MDH_ERR_SIZE),
- *            one for each 128 or 64 columns of each of the B * H states, in the backward call of three passes.
+ *            0 <= B, 0 <= T < 2^31 - 64, the others >= 1, dk and dv <= 256.  A call has fewer than 2^24 workgroups
+ *            (MDH_ERR_SIZE), one for each 128 or 64 columns of each of the B * H states, in the backward call of three passes.
  *   q, k, v  (B, T, Hq, dk), (B, T, Hk, dk), (B, T, Hv, dv); o: (B, T, H, dv); of type dtype
  *   strides  12 numbers, (batch, token, head) of q, k, v, o in elements; channels are adjacent.
  *            NULL: all dense.  Inputs may have stride 0 (one value for all), and 64 tokens lie within 2^31

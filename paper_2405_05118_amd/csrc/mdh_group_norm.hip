@@ -12,11 +12,12 @@
 // Sums over shares are taken in a fixed order.  Gradients of weight and bias: one row of the workspace for each share, summed
 // by the workgroups of the second launch that come after those for the images (teams: a launch of their own).
 //
-// Measured, bf16 unless said (inputs not in the caches).  Teams: 16384 rows of 4096 in 32 groups with a gate 81 us (5.0 TB/s),
-// their gradients 152 + 5 (4.4 TB/s; with 1024 workgroups 139 + 7); one such row 3.2.  Slabs: 8 x 128 x 128 x 256 in 32 groups, silu, 15 + 37 us (67 MB read,
-// read again and written: 3.9 TB/s), gradients 46 + 57; fp32 16 x 56 x 56 x 64 in 32 groups 7 + 11.  Stores that leave the
-// caches alone are up to a tenth faster (16384 rows, trained: 5 %) and cost whoever reads the output next as much
-// (2048 rows and a sum after it: 20.1 us for 19.5): not taken.
+// Measured, bf16 unless said, three sets of inputs in turn.  Teams: 16384 rows of 4096 in 32 groups with a gate 77 us (5.2 TB/s),
+// their gradients 148 (4.5 TB/s over five tensors); one such row 3.4 in its kernel.  Slabs: 8 x 128 x 128 x 256 in 32 groups, silu,
+// 51 us (67 MB read, read again and written: 3.9 TB/s), trained 143, of which a kernel trace gives 24 + 31 to the forward call and 43 +
+// 47 to the gradients; fp32 16 x 56 x 56 x 64 in 32 groups 17 (7 + 11).  Stores that leave the caches alone are up to a
+// tenth faster (16384 rows, trained: 5 %) and cost whoever reads the output next as much (2048 rows and a sum after it: 20.1 us for
+// 19.5): not taken.
 #include "mdh_act.h"
 #include "mdh_internal.h"
 #include "mdh_types.h"
@@ -647,7 +648,8 @@ __global__ __launch_bounds__(kLanes) void slabs_backward_kernel(GroupNormCall c,
 
 int bytes_of(const GroupNormCall& c) { return c.dtype == MDH_BF16 ? 2 : 4; }
 
-// Channels of a lane's access for D channels a group: what divides them, of 16 bytes at most.
+// Channels of a lane's access for D channels a group: what divides them, of 16 bytes at most.  (No access of 8 bytes for bf16: groups
+// of a multiple of 4 channels, but not of 8, take 4 bytes.  4096 rows of 16 groups of 100 channels 22 us, of 104 12.)
 int widest(int D, int bytes) {
   for (int v : {8, 4, 2})
     if (v * bytes <= 16 && D % v == 0 && !(bytes == 2 && v == 4)) return v;
@@ -664,9 +666,12 @@ int width(const GroupNormCall& c, bool backward) {
   return v;
 }
 
+// Rows of wider groups go as images of one position, each with its own sums for the gradients of weight and bias: 16384 rows of 4096 as
+// one group, bf16 with a gate, 259 us, trained 1180 with 541 MB of workspace.
 bool use_teams(const GroupNormCall& c, int V) { return c.S == 1 && c.C / c.G / V <= 256; }
 
-// pieces of a lane
+// pieces of a lane (four: the backward call has one wavefront a SIMD; trained, with a gate, 2048 rows of 4096 in 2 groups take 65 us,
+// in 32 groups 42)
 int pieces(const GroupNormCall& c, int V) {
   const int P = c.C / c.G / V;
   return P <= 64 ? 1 : P <= 128 ? 2 : 4;
@@ -682,8 +687,8 @@ Teams teams_of(const GroupNormCall& c, int V, bool backward) {
   const int64_t slabs = cdiv(c.G, t.across), step = kLanes / (t.L * t.across);
   // Workgroups.  Forward: four goes each, within 1024 to 8192 (16384 rows of 4096 with a gate: 8192 79-81 us, 2048 88-90, 16384 86;
   // 2048 rows: 1024 12.9 us, 2048 13.9, 8192 14.7).  In the backward call each leaves a row of the workspace, which a launch
-  // adds up: two a compute unit (gradients and forward, 4096 rows of 2048: 512 47 us, 1024 55, 256 51; 16384 rows of 4096 236,
-  // 239, 303).
+  // adds up: two a compute unit (256 / 512 / 1024 workgroups, the backward call, bf16 with a gate: 16384 rows of 4096 215 / 148 / 152 us
+  // -- with the forward call before it 284 / 227 / 223 --, 4096 of 2048 33 / 30 / 39, 2048 of 4096 32 / 28 / 32).
   const int64_t goes = slabs * cdiv(c.N, step), most_wg = goes / 4 < 1024 ? 1024 : goes / 4 > 8192 ? 8192 : goes / 4;
   int64_t shares = (backward ? 512 : most_wg) / slabs;
   if (shares < 1) shares = 1;

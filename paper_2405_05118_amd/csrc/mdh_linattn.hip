@@ -18,10 +18,11 @@
 // lost).  bf16 operands are one slice; scores and S are rounded to one slice where they are operands (2^-9 of a
 // term, as the output's own rounding), but what is added to S is not: c_j times its decay is three slices.
 //
-// Bound by memory where the sequence is long: 65536 x 16 heads of 128 x 128, bf16, 130 us for the states of 32 segments (4.1
-// TB/s; 122 without its arithmetic), 15 for their prefix sum and 240-250 for the pass (4.4 TB/s, 280 TFLOP/s).  2048 x 32
-// heads: 15 + 8 + 28 us, the last for four runs of a workgroup one after the other.  Trained, 8 x 4096 x 16 heads: 71 + 11 +
-// 140 for the forward call, 440-470 for the three passes of the backward call, which read nine tensors and write three.
+// Bound by memory where the sequence is long: 65536 x 16 heads of 128 x 128, bf16, 390 us a call; in a kernel trace, whose sums
+// are up to a tenth more, 142 for the states of 32 segments (3.8 TB/s; its arithmetic taken out, 122 of 131 were left), 15 for
+// their prefix sum and 271 for the pass (4.0 TB/s, 253 TFLOP/s).  2048 x 32 heads: 48 us, 15 + 8 + 29, the last for four runs
+// of a workgroup one after the other.  Trained, 8 x 4096 x 16 heads: 590 us, 64 + 10 + 127 for the forward call and 407 for
+// the three passes of the backward call, which read nine tensors and write three.
 #include "mdh_internal.h"
 #include "mdh_types.h"
 
@@ -118,7 +119,8 @@ constexpr int kWaves = 4, kThreads = 64 * kWaves;
 // How rows are read and written (one kernel for each: what the general ones keep in registers would cost the first its speed).
 //   kVec   16 bytes at a time: bases, strides and rows are multiples of 16 bytes
 //   kAny   16 bytes at a time at any address; the row's last ones are read as the 16 bytes that end with it and moved down
-//          (rows have 16 bytes at least)
+//          (rows have 16 bytes at least).  The bf16 passes keep 52 to 72 bytes a lane in scratch: 4 x 2048 x 16 heads of 100 x 90,
+//          93 us, trained 302, where 104 x 96 aligned take 70 and 196.
 //   kEach  element by element: shorter rows
 enum Access { kVec = 0, kAny = 1, kEach = 2 };
 

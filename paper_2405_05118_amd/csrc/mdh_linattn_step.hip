@@ -8,7 +8,8 @@
 // its own out (cached / not, the states cold: 32 of 128 x 128 4.4 / 4.0 us, 512 17.3 / 12.4, 1024 32.3 / 26.0, 4096 113.7 /
 // 102.4 = 5.2 TB/s; of one layer called again and again 3.8 / 3.8, 10.5 / 10.0, 24.8 / 22.8, 89.6 / 101.8).
 // Measured in a graph, W = 64 / 16, states of 128 x 128: 32 of them 5.3 / 4.0 us, 128 6.3 / 6.1, 256 7.9 / 11.8, 1024
-// 26.0 / 47.1; W = 128: 9.7, 10.8, 12.6, 25.4.
+// 26.0 / 47.1; W = 128: 9.7, 10.8, 12.6, 25.4.  Where dv is no multiple of 4, or the states are not 16-byte aligned, a lane has one
+// column and W is 16: 250 x 16 states of 128 x 127 501 us.
 #include "mdh_internal.h"
 #include "mdh_types.h"
 
