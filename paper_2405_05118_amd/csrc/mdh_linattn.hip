@@ -530,7 +530,7 @@ __global__ __launch_bounds__(kThreads, ACCESS == kEach ? 2 : KP == 64 && NB == 1
     // the next run's operands take the place of this one's, of which only the scores are still asked for
     store(pos + next);
     if (STATE && n < C) update_weights(C);
-    load(pos + 2 * next);
+    load((int)((uint32_t)pos + 2u * (uint32_t)next));  // (past 2^31: negative, and nothing to load)
     if constexpr (!STATE) {
       // what the run's own positions give
 #pragma unroll
