@@ -721,7 +721,8 @@ Slabs slabs_of(const GroupNormCall& c, int V) {
   const int at_once = 16 * (kLanes / s.groups) / s.per_group;
   if (shares > at_once) shares = at_once;
   if (shares < 1) shares = 1;
-  if (shares == 1 && c.S > 1 << 30) shares = 2;  // (a share's positions, and kBatch * kLanes more, are counted in 32 bits)
+  // (A share's positions, and kBatch * kLanes more, are counted in 32 bits: images of 2^30 positions that fit the memory have fewer than
+  // 256 channels, one slab, and so 16 shares at least.)
   s.rows = (int)cdiv(c.S, shares);
   s.shares = (int)cdiv(c.S, s.rows);
   return s;
