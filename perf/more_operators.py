@@ -443,7 +443,8 @@ def _plain_norm(s):
 def _workspace(s, bytes_):
     """What the caller keeps between calls."""
     if "workspace" not in s:
-        s["workspace"] = torch.empty(bytes_(), dtype=torch.uint8, device="cuda") if bytes_() else None
+        n = bytes_()
+        s["workspace"] = torch.empty(n, dtype=torch.uint8, device="cuda") if n else None
     return s["workspace"]
 
 
@@ -454,17 +455,21 @@ def _own_scan(s):
     train = c["kind"] == "scan_train"
     sizes = tuple(c[n] for n in ("B", "T", "D", "N", "G"))
     ws = _workspace(s, lambda: mdh.mdh_selective_scan_workspace_size(sizes, s["x"].dtype, backward=train))
+    if train and "checkpoints" not in s:  # what the forward call leaves for the backward call: states along the tokens
+        s["checkpoints"] = torch.empty(mdh.mdh_selective_scan_checkpoints_size(sizes), dtype=torch.uint8, device="cuda")
+    kept = s.get("checkpoints")
     mdh.mdh_selective_scan(s["x"], s["dt"], s["A"], s["b"], s["c"], s["y"], skip=s["skip"], gate=s["gate"], dt_bias=s["dt_bias"],
-                           softplus=True, lengths=s["lengths"], initial_state=s["initial"], final_state=s["final"], workspace=ws)
+                           softplus=True, lengths=s["lengths"], initial_state=s["initial"], final_state=s["final"], checkpoints=kept,
+                           workspace=ws)
     got = {"y": s["y"]}
     if s["final"] is not None:
         got["final"] = s["final"]
     if not train:
         return got
     mdh.mdh_selective_scan_backward(s["x"], s["dt"], s["A"], s["b"], s["c"], s["d_y"], s["d_x"], s["d_dt"], s["d_A"], s["d_b"], s["d_c"],
-                                    skip=s["skip"], gate=s["gate"], dt_bias=s["dt_bias"], softplus=True, lengths=s["lengths"],
-                                    initial_state=s["initial"], d_final_state=s["d_final"], d_skip=s["d_skip"], d_gate=s["d_gate"],
-                                    d_dt_bias=s["d_dt_bias"], d_initial_state=s["d_initial"], workspace=ws)
+                                    kept, skip=s["skip"], gate=s["gate"], dt_bias=s["dt_bias"], softplus=True, lengths=s["lengths"],
+                                    d_final_state=s["d_final"], d_skip=s["d_skip"], d_gate=s["d_gate"], d_dt_bias=s["d_dt_bias"],
+                                    d_initial_state=s["d_initial"], workspace=ws)
     got.update((n, s[n]) for n in ("d_x", "d_dt", "d_b", "d_c", "d_A", "d_skip", "d_dt_bias"))
     got.update((n, s[n]) for n in ("d_gate", "d_initial") if s[n] is not None)
     return got
