@@ -488,8 +488,8 @@ def _own_conv(s):
 
     c = s["case"]
     act = getattr(mdh, "MDH_ACT_" + c["act"].upper())
-    mdh.mdh_causal_conv(s["x"], s["weight"], s["bias"], s["y"], act, lengths=s["lengths"], initial_state=s["initial"],
-                        final_state=s["final"])
+    mdh.mdh_causal_conv(s["x"], s["weight"], s["bias"], s["y"], act, lengths=s["lengths"], initial_window=s["initial"],
+                        final_window=s["final"])
     got = {"y": s["y"]}
     if s["final"] is not None:
         got["final"] = s["final"]
@@ -497,8 +497,8 @@ def _own_conv(s):
         return got
     ws = _workspace(s, lambda: mdh.mdh_causal_conv_workspace_size(tuple(c[n] for n in ("B", "T", "C", "W")), s["x"].dtype))
     mdh.mdh_causal_conv_backward(s["x"], s["weight"], s["bias"], s["d_y"], s["d_x"], s["d_weight"], s["d_bias"], act,
-                                 lengths=s["lengths"], initial_state=s["initial"], d_final_state=s["d_final"],
-                                 d_initial_state=s["d_initial"], workspace=ws)
+                                 lengths=s["lengths"], initial_window=s["initial"], d_final_window=s["d_final"],
+                                 d_initial_window=s["d_initial"], workspace=ws)
     got.update((n, s[n]) for n in ("d_x", "d_weight", "d_bias"))
     if s["d_initial"] is not None:
         got["d_initial"] = s["d_initial"]
