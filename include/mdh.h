@@ -593,6 +593,139 @@ mdh_status mdh_group_norm_backward(const int64_t* sizes, mdh_dtype dtype, const 
                                    const float* mean, const float* rstd, int32_t act, void* d_x, void* d_gate,
                                    float* d_weight, float* d_bias, void* workspace, size_t workspace_bytes, void* stream);
 
+/* ------------------------------------------------------------------------- */
+/* A selective state space block: short causal convolution, scan, layer norm   */
+/* ------------------------------------------------------------------------- */
+
+/*
+ * A causal convolution along the tokens with a filter for each channel:
+ *   y_t[ch] = act(bias[ch] + sum_{j<W} weight[ch][j] X_{t-W+1+j}[ch])   for every batch entry b, token t < lengths[b],
+ * X_t the token t of x, and for t < 0 row W - 1 + t of the window that came in (zeros without one):
+ * md_hom(*, (++, ++, ++, +)) over (b, t, ch, j), mdh_mcc's index function t + j with no dimension over channels.
+ *   sizes    (B, T, C, W): 0 <= B, 0 <= T < 2^31 - 64, B * T < 2^31, 1 <= C < 2^24, 1 <= W <= 8 (MDH_ERR_UNSUPPORTED).
+ *            A call has fewer than 2^32 - 256 lanes (MDH_ERR_SIZE), one for 16 bytes of the channels of 8 to 64 tokens.
+ *   x, y     (B, T, C) of type dtype; strides: 4 numbers, (batch, token) of x, y in elements, channels adjacent;
+ *            NULL: dense.  Any alignment that the type has.  y does not overlap x.
+ *   weight   (C, W) fp32; bias: C fp32 or NULL (zeros); act: MDH_ACT_*
+ *   lengths  B int32 or NULL (all T).  Tokens from lengths[b] on are not read (any value, NaN too); their outputs
+ *            are 0.  Less than 0 counts as 0, more than T as T.
+ *   initial_window, final_window  (B, W - 1, C) of type dtype: the last W - 1 rows of X before the first token, and up to
+ *            the length.  NULL: zeros / not wanted.  They may be the same buffer.  With slots (B int32) they are pools of
+ *            n_slots windows, and batch entry b has that of slots[b]; outside of [0, n_slots) it has none: zeros,
+ *            none written.  The slots of one call are distinct.
+ * Sums are fp32.
+ */
+mdh_status mdh_causal_conv(const int64_t* sizes, mdh_dtype dtype, const void* x, const int64_t* strides, const float* weight,
+                           const float* bias, int32_t act, const int32_t* lengths, const void* initial_window,
+                           void* final_window, const int32_t* slots, int64_t n_slots, void* y, void* stream);
+/*
+ * Gradients of mdh_causal_conv from those of y and of the final window (NULL: zeros).
+ *   strides  6 numbers, (batch, token) of x, d_y, d_x; NULL: dense.  d_x does not overlap x or d_y.
+ *   initial_window  what the forward call had (without slots); d_initial_window: NULL = not wanted
+ *   d_weight, d_bias  (C, W) and C fp32 or NULL; summed over all tokens in a fixed order
+ *   workspace  mdh_causal_conv_workspace_size(sizes, dtype) bytes, 16-byte aligned
+ * relu's slope at 0 is 0.
+ */
+size_t mdh_causal_conv_workspace_size(const int64_t* sizes, mdh_dtype dtype);
+mdh_status mdh_causal_conv_backward(const int64_t* sizes, mdh_dtype dtype, const void* x, const void* d_y, const int64_t* strides,
+                                    const float* weight, const float* bias, int32_t act, const int32_t* lengths,
+                                    const void* initial_window, const void* d_final_window, void* d_x, void* d_initial_window,
+                                    float* d_weight, float* d_bias, void* workspace, size_t workspace_bytes, void* stream);
+/*
+ * One token of mdh_causal_conv with the window in place: it moves on by the token.
+ *   sizes    (B, C, W);  x, y: (B, C);  strides: 2 numbers, batch of x, y; NULL: dense
+ *   window   (B, W - 1, C) of type dtype, read and written; with slots a pool of n_slots of them, as above: a batch
+ *            entry without a slot has y = 0.  (W = 1: none, any pointer.)
+ */
+mdh_status mdh_causal_conv_step(const int64_t* sizes, mdh_dtype dtype, const void* x, const int64_t* strides, const float* weight,
+                                const float* bias, int32_t act, void* window, const int32_t* slots, int64_t n_slots, void* y,
+                                void* stream);
+
+/*
+ * The selective state space scan.  For every batch entry b, channel ch (of group g = ch / (D / G)) and state n < N:
+ *   delta_t = softplus(dt_t + dt_bias)           (softplus = 0: dt_t + dt_bias itself)
+ *   h_t[n] = exp(delta_t A[ch][n]) h_{t-1}[n] + delta_t x_t b_t[g][n]
+ *   y_t = (sum_n c_t[g][n] h_t[n] + skip[ch] x_t) silu(gate_t)          for t < lengths[b]
+ * -- the prefix-sum operator on pairs, (a1, u1) op (a2, u2) = (a1 a2, a2 u1 + u2) (paper: Appendix, Example "Prefix-Sum"), with a
+ * factor that every token gives, where mdh_linattn's is a constant of the head.
+ *   sizes    (B, T, D, N, G): 0 <= B, 0 <= T < 2^31 - 64, B * T < 2^31, 1 <= D < 2^24, 1 <= N <= 64 (MDH_ERR_UNSUPPORTED), G divides
+ *            D, B * T * G * N < 2^32.  A call has fewer than 2^24 workgroups, backward 2^23 (MDH_ERR_SIZE): one for each 16
+ *            (backward: 64) channels of a group and batch entry.
+ *   x, dt, gate, y  (B, T, D) of type dtype; gate: NULL = no gate.  b, c: (B, T, G, N).
+ *   strides  14 numbers: (batch, token) of x, dt, gate, y, then (batch, token, group) of b, c, in elements; channels and
+ *            states are adjacent; NULL: all dense.  Inputs may have stride 0.  Any alignment that the type has.  y may be dt
+ *            or gate (the same elements), and overlaps no other input.
+ *   A        (D, N) fp32, finite; skip, dt_bias: D fp32 or NULL (zeros)
+ *   lengths  as of mdh_causal_conv
+ *   initial_state, final_state  (B, D, N) fp32; NULL: zeros / not wanted.  They may be the same buffer.  With slots pools of
+ *            n_slots states, as of mdh_causal_conv.
+ *   checkpoints  mdh_selective_scan_checkpoints_size(sizes) bytes for the backward call, 16-byte aligned, or NULL: states every 16
+ *            tokens, 4 N / 16 bytes a token and channel
+ *   workspace  mdh_selective_scan_workspace_size(sizes, dtype, 0) bytes, 16-byte aligned (NULL where that is 0)
+ * States and sums are fp32.
+ */
+size_t mdh_selective_scan_workspace_size(const int64_t* sizes, mdh_dtype dtype, int32_t backward);
+size_t mdh_selective_scan_checkpoints_size(const int64_t* sizes);
+mdh_status mdh_selective_scan(const int64_t* sizes, mdh_dtype dtype, const void* x, const void* dt, const void* gate, const void* b,
+                              const void* c, const int64_t* strides, const float* A, const float* skip, const float* dt_bias,
+                              int32_t softplus, const int32_t* lengths, const float* initial_state, float* final_state,
+                              const int32_t* slots, int64_t n_slots, void* y, void* checkpoints, size_t checkpoints_bytes,
+                              void* workspace, size_t workspace_bytes, void* stream);
+/*
+ * Gradients of mdh_selective_scan from those of y and of the final state (NULL: zeros), and from the forward call's checkpoints
+ * (which hold the initial state too).
+ *   strides  26 numbers: (batch, token) of x, dt, gate, d_y, d_x, d_dt, d_gate, then (batch, token, group) of b, c, d_b, d_c;
+ *            NULL: all dense.  Gradients of the activations overlap no input and are wanted all, d_gate where there is a gate.
+ *   d_A, d_skip, d_dt_bias, d_initial_state  fp32, NULL: not wanted
+ *   workspace  mdh_selective_scan_workspace_size(sizes, dtype, 1) bytes, which hold what the forward call wants too
+ * Sums over channels (d_b, d_c) and over tokens (d_A, d_skip, d_dt_bias) are fp32, in a fixed order.
+ */
+mdh_status mdh_selective_scan_backward(const int64_t* sizes, mdh_dtype dtype, const void* x, const void* dt, const void* gate,
+                                       const void* b, const void* c, const void* d_y, const int64_t* strides, const float* A,
+                                       const float* skip, const float* dt_bias, int32_t softplus, const int32_t* lengths,
+                                       const float* d_final_state, const void* checkpoints, size_t checkpoints_bytes, void* d_x,
+                                       void* d_dt, void* d_gate, void* d_b, void* d_c, float* d_A, float* d_skip, float* d_dt_bias,
+                                       float* d_initial_state, void* workspace, size_t workspace_bytes, void* stream);
+/*
+ * One token of mdh_selective_scan with the state in place.
+ *   sizes    (B, D, N, G), B * D < 2^25;  x, dt, gate, y: (B, D);  b, c: (B, G, N)
+ *   strides  8 numbers: batch of x, dt, gate, y, then (batch, group) of b, c; NULL: all dense
+ *   state    (B, D, N) fp32, read and written; with slots a pool of n_slots of them: a batch entry without a slot has
+ *            y = 0.  Pools may pass 2^31 elements.
+ */
+mdh_status mdh_selective_scan_step(const int64_t* sizes, mdh_dtype dtype, const void* x, const void* dt, const void* gate,
+                                   const void* b, const void* c, const int64_t* strides, const float* A, const float* skip,
+                                   const float* dt_bias, int32_t softplus, float* state, const int32_t* slots, int64_t n_slots,
+                                   void* y, void* stream);
+
+/*
+ * Layer norm of rows of C channels, with the sum of a residual stream in front of it:
+ *   s = x + residual  (rounded to dtype; without a residual s = x),  y = (s - mean) * rstd * weight + bias,  rstd = 1 / sqrt(variance + eps)
+ * -- mdh_group_norm's rows as one group, for rows of any width.
+ *   sizes    (rows, C): 0 <= rows < 2^31, 1 <= C < 2^24; fewer than 2^24 workgroups (rows of more than 256 accesses of 16 bytes have
+ *            one each, of more than 1024 at most 2^22 - 1 of four times the size: MDH_ERR_SIZE)
+ *   x, residual, total, y  rows of type dtype; row_strides: 4 numbers, elements from row to row of x, residual, total, y; NULL:
+ *            dense.  Any alignment that the type has.  residual: NULL, or total receives s (x, residual or a buffer of its own).
+ *            y may be x where there is no residual.
+ *   weight, bias  C fp32, or NULL (1 and 0);  mean, rstd: rows fp32 each, or NULL: what the backward call wants
+ * Variances are sums of squared differences from the mean, in fp32; one value in all of a row gives bias.  Inf or NaN in a row
+ * makes that row NaN and no other.
+ */
+mdh_status mdh_layer_norm(const int64_t* sizes, mdh_dtype dtype, const void* x, const void* residual, const int64_t* row_strides,
+                          const float* weight, const float* bias, float eps, void* total, void* y, float* mean, float* rstd,
+                          void* stream);
+/*
+ * Gradients of mdh_layer_norm.  s: what was normalised (total, or x);  d_total: the gradient of s from elsewhere, NULL: none;
+ *   d_s = d_total + rstd (t - mean(t) - sh mean(t sh)),  t = d_y weight, sh = (s - mean) rstd: the gradient of x and of the residual
+ *   row_strides  4 numbers, of s, d_y, d_total, d_s; NULL: dense.  d_s may be d_y or d_total.
+ *   d_weight, d_bias  C fp32 or NULL; summed over the rows in a fixed order
+ *   workspace  mdh_layer_norm_workspace_size(sizes, dtype) bytes, 16-byte aligned
+ */
+size_t mdh_layer_norm_workspace_size(const int64_t* sizes, mdh_dtype dtype);
+mdh_status mdh_layer_norm_backward(const int64_t* sizes, mdh_dtype dtype, const void* s, const void* d_y, const void* d_total,
+                                   const int64_t* row_strides, const float* weight, const float* mean, const float* rstd, void* d_s,
+                                   float* d_weight, float* d_bias, void* workspace, size_t workspace_bytes, void* stream);
+
 /*
  * Small per-workload tile-parameter search (paper: Section "Auto-Tuning", with
  * the search space shrunk to this library's kernel instantiations): runs every

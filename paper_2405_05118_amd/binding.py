@@ -175,6 +175,23 @@ def lib() -> ctypes.CDLL:
         L.mdh_group_norm_workspace_size.argtypes = [packed, ctypes.c_int, i32]
         L.mdh_group_norm.argtypes = [packed, ctypes.c_int, vp, vp, packed, vp, vp, f32, i32, vp, vp, vp, vp, sz, vp]
         L.mdh_group_norm_backward.argtypes = [packed, ctypes.c_int, vp, vp, vp, packed, vp, vp, vp, vp, i32, vp, vp, vp, vp, vp, sz, vp]
+        L.mdh_causal_conv_workspace_size.restype = sz
+        L.mdh_causal_conv_workspace_size.argtypes = [packed, ctypes.c_int]
+        L.mdh_causal_conv.argtypes = [packed, ctypes.c_int, vp, packed, vp, vp, i32, vp, vp, vp, vp, i64, vp, vp]
+        L.mdh_causal_conv_backward.argtypes = [packed, ctypes.c_int, vp, vp, packed, vp, vp, i32, vp, vp, vp, vp, vp, vp, vp, vp, sz, vp]
+        L.mdh_causal_conv_step.argtypes = [packed, ctypes.c_int, vp, packed, vp, vp, i32, vp, vp, i64, vp, vp]
+        L.mdh_selective_scan_workspace_size.restype = sz
+        L.mdh_selective_scan_workspace_size.argtypes = [packed, ctypes.c_int, i32]
+        L.mdh_selective_scan_checkpoints_size.restype = sz
+        L.mdh_selective_scan_checkpoints_size.argtypes = [packed]
+        L.mdh_selective_scan.argtypes = ([packed, ctypes.c_int] + [vp] * 5 + [packed, vp, vp, vp, i32] + [vp] * 4 + [i64, vp, vp, sz, vp, sz, vp])
+        L.mdh_selective_scan_backward.argtypes = ([packed, ctypes.c_int] + [vp] * 6 + [packed, vp, vp, vp, i32, vp, vp, vp, sz] + [vp] * 9
+                                                  + [vp, sz, vp])
+        L.mdh_selective_scan_step.argtypes = [packed, ctypes.c_int] + [vp] * 5 + [packed, vp, vp, vp, i32, vp, vp, i64, vp, vp]
+        L.mdh_layer_norm_workspace_size.restype = sz
+        L.mdh_layer_norm_workspace_size.argtypes = [packed, ctypes.c_int]
+        L.mdh_layer_norm.argtypes = [packed, ctypes.c_int, vp, vp, packed, vp, vp, f32, vp, vp, vp, vp, vp]
+        L.mdh_layer_norm_backward.argtypes = [packed, ctypes.c_int, vp, vp, vp, packed, vp, vp, vp, vp, vp, vp, vp, sz, vp]
         L.mdh_num_candidates.restype = i32
         L.mdh_num_candidates.argtypes = [ctypes.c_int, p64]
         L.mdh_candidate.argtypes = [ctypes.c_int, p64, i32, pp]
@@ -408,7 +425,7 @@ def mdh_matvec(A, x, y, params: Optional[TileParams] = None, workspace=None):
 # Sizes and strides cross the ABI as bytes of int64: packing them takes a fifth of the time that filling a ctypes array does,
 # and a token's group norm or step is as fast as the host is (of 10 us a call 4 are left).
 
-_q4, _q7, _q8 = (struct.Struct("%dq" % n).pack for n in (4, 7, 8))
+_q2, _q3, _q4, _q5, _q7, _q8 = (struct.Struct("%dq" % n).pack for n in (2, 3, 4, 5, 7, 8))
 
 
 def _dtype_of(dtype) -> int:
@@ -445,15 +462,19 @@ def _strides(tensors):
     return None
 
 
-def _states(B, H, dk, dv, slots, *named):
+def _pools(B, each, dtype, slots, *named):
     """The states' pointers, number of slots and slots' pointer; with slots they are pools of any size."""
     n = 0
     if slots is not None:
         n = max((t.shape[0] for t, _ in named if t is not None), default=0)
         if any(t is not None and t.shape[0] != n for t, _ in named):
             raise ValueError("the pools of states have different numbers of slots")
-    shape = (B if slots is None else n, H, dk, dv)
-    return [_opt(t, _F32, name, shape) for t, name in named], n, _opt(slots, _I32, "slots", (B,))
+    shape = (B if slots is None else n, *each)
+    return [_opt(t, dtype, name, shape) for t, name in named], n, _opt(slots, _I32, "slots", (B,))
+
+
+def _states(B, H, dk, dv, slots, *named):
+    return _pools(B, (H, dk, dv), _F32, slots, *named)
 
 
 def _unfit(*named):
@@ -597,6 +618,212 @@ def mdh_group_norm_backward(x, weight, bias, mean, rstd, d_y, d_x, d_weight, d_b
                                    _opt(mean, _F32, "mean", (N, groups)), _opt(rstd, _F32, "rstd", (N, groups)), act, dxp, dgp,
                                    _opt(d_weight, _F32, "d_weight", (C,)), _opt(d_bias, _F32, "d_bias", (C,)), wp, wb, _stream())
     _check(st, "mdh_group_norm_backward")
+    return d_x
+
+
+# ------------------------------------------------------------------ a selective state space block
+
+
+def _same(shape, *named):
+    for t, name in named:
+        if t is not None and t.shape != shape:
+            raise ValueError("%s has shape %s, not %s" % (name, tuple(t.shape), tuple(shape)))
+
+
+def _sp(t, dtype, name):
+    return None if t is None else _strided(t, dtype, name)
+
+
+def mdh_causal_conv(x, weight, bias, y, act: int = MDH_ACT_NONE, lengths=None, initial_window=None, final_window=None, slots=None):
+    """y[b,t] = act(bias + sum_j weight[:,j] X[b,t-W+1+j]), X the window that came in and the tokens of x behind it.
+
+    x, y: (B, T, C), any strides with adjacent channels; weight: (C, W) float32; bias: (C,) float32 or None; lengths: (B,) int32;
+    windows: (B, W - 1, C) of x's type, or with slots (B,) int32 pools (n, W - 1, C)."""
+    L = _lib or lib()
+    B, T, C = x.shape
+    W = weight.shape[1]
+    _same(x.shape, (y, "y"))
+    dt = x.dtype
+    d = _dtype_of(dt)
+    (wi, wo), n, slots_p = _pools(B, (W - 1, C), dt, slots, (initial_window, "initial_window"), (final_window, "final_window"))
+    st = L.mdh_causal_conv(_q4(B, T, C, W), d, _strided(x, dt, "x"), _strides((x, y)), _opt(weight, _F32, "weight", (C, W)),
+                           _opt(bias, _F32, "bias", (C,)), act, _opt(lengths, _I32, "lengths", (B,)), wi, wo, slots_p, n,
+                           _strided(y, dt, "y"), _stream())
+    _check(st, "mdh_causal_conv")
+    return y
+
+
+def mdh_causal_conv_workspace_size(sizes: Sequence[int], dtype) -> int:
+    """Of the backward call.  ``sizes``: (B, T, C, W); ``dtype``: torch.float32 or torch.bfloat16."""
+    return int(lib().mdh_causal_conv_workspace_size(_q4(*sizes), _dtype_of(dtype)))
+
+
+def mdh_causal_conv_backward(x, weight, bias, d_y, d_x, d_weight, d_bias, act: int = MDH_ACT_NONE, lengths=None, initial_window=None,
+                             d_final_window=None, d_initial_window=None, workspace=None):
+    """Gradients of mdh_causal_conv; d_weight: (C, W), d_bias: (C,) float32, or None."""
+    L = _lib or lib()
+    B, T, C = x.shape
+    W = weight.shape[1]
+    _same(x.shape, (d_y, "d_y"), (d_x, "d_x"))
+    dt = x.dtype
+    d = _dtype_of(dt)
+    (wi, dwo, dwi), _, _ = _pools(B, (W - 1, C), dt, None, (initial_window, "initial_window"), (d_final_window, "d_final_window"),
+                                  (d_initial_window, "d_initial_window"))
+    wp, wb = _ws(workspace)
+    st = L.mdh_causal_conv_backward(_q4(B, T, C, W), d, _strided(x, dt, "x"), _strided(d_y, dt, "d_y"), _strides((x, d_y, d_x)),
+                                    _opt(weight, _F32, "weight", (C, W)), _opt(bias, _F32, "bias", (C,)), act,
+                                    _opt(lengths, _I32, "lengths", (B,)), wi, dwo, _strided(d_x, dt, "d_x"), dwi,
+                                    _opt(d_weight, _F32, "d_weight", (C, W)), _opt(d_bias, _F32, "d_bias", (C,)), wp, wb, _stream())
+    _check(st, "mdh_causal_conv_backward")
+    return d_x
+
+
+def mdh_causal_conv_step(x, weight, bias, window, y, act: int = MDH_ACT_NONE, slots=None):
+    """One token with the window in place.  x, y: (B, C); window: (B, W - 1, C), or with slots (B,) int32 a pool (n, W - 1, C)."""
+    L = _lib or lib()
+    B, C = x.shape
+    W = weight.shape[1]
+    _same(x.shape, (y, "y"))
+    dt = x.dtype
+    d = _dtype_of(dt)
+    (wp,), n, slots_p = _pools(B, (W - 1, C), dt, slots, (window, "window"))
+    st = L.mdh_causal_conv_step(_q3(B, C, W), d, _strided(x, dt, "x"), _strides((x, y)), _opt(weight, _F32, "weight", (C, W)),
+                                _opt(bias, _F32, "bias", (C,)), act, wp, slots_p, n, _strided(y, dt, "y"), _stream())
+    _check(st, "mdh_causal_conv_step")
+    return y
+
+
+def mdh_selective_scan_workspace_size(sizes: Sequence[int], dtype, backward: bool = False) -> int:
+    """``sizes``: (B, T, D, N, G); ``dtype``: torch.float32 or torch.bfloat16."""
+    return int(lib().mdh_selective_scan_workspace_size(_q5(*sizes), _dtype_of(dtype), int(backward)))
+
+
+def mdh_selective_scan_checkpoints_size(sizes: Sequence[int]) -> int:
+    """Bytes that the forward call leaves for the backward call.  ``sizes``: (B, T, D, N, G)."""
+    return int(lib().mdh_selective_scan_checkpoints_size(_q5(*sizes)))
+
+
+def _scan_operands(lead, x, A, b, c, dt, *alike):
+    """Sizes behind the leading ones; every tensor of ``alike`` has x's shape, b and c (*lead, G, N)."""
+    D, N = A.shape
+    if x.shape != (*lead, D):
+        raise _unfit(("x", x), ("A", A))
+    if len(b.shape) != len(lead) + 2 or b.shape[:-2] != lead or b.shape[-1] != N or c.shape != b.shape:
+        raise _unfit(("A", A), ("b", b), ("c", c))
+    _same(x.shape, (dt, "dt"), *alike)
+    return D, N, b.shape[-2]
+
+
+def mdh_selective_scan(x, dt, A, b, c, y, skip=None, gate=None, dt_bias=None, softplus: bool = False, lengths=None, initial_state=None,
+                       final_state=None, slots=None, checkpoints=None, workspace=None):
+    """h[t] = exp(delta[t] A) h[t-1] + delta[t] x[t] b[t], y[t] = (sum_n c[t] h[t] + skip x[t]) silu(gate[t]), with delta = dt + dt_bias,
+    or softplus of it.
+
+    x, dt, gate, y: (B, T, D), b, c: (B, T, G, N), any strides with adjacent channels; A: (D, N), skip, dt_bias: (D,) float32;
+    lengths: (B,) int32; states: (B, D, N) float32, or with slots (B,) int32 pools (n, D, N); checkpoints: a buffer of
+    mdh_selective_scan_checkpoints_size bytes, what the backward call wants."""
+    L = _lib or lib()
+    B, T = lead = x.shape[:2]
+    D, N, G = _scan_operands(lead, x, A, b, c, dt, (y, "y"), (gate, "gate"))
+    ty = x.dtype
+    d = _dtype_of(ty)
+    (si, so), n, slots_p = _pools(B, (D, N), _F32, slots, (initial_state, "initial_state"), (final_state, "final_state"))
+    (cp, cb), (wp, wb) = _ws(checkpoints), _ws(workspace)
+    st = L.mdh_selective_scan(_q5(B, T, D, N, G), d, _strided(x, ty, "x"), _strided(dt, ty, "dt"), _sp(gate, ty, "gate"),
+                              _strided(b, ty, "b"), _strided(c, ty, "c"), _strides((x, dt, x if gate is None else gate, y, b, c)),
+                              _opt(A, _F32, "A"), _opt(skip, _F32, "skip", (D,)), _opt(dt_bias, _F32, "dt_bias", (D,)), int(softplus),
+                              _opt(lengths, _I32, "lengths", (B,)), si, so, slots_p, n, _strided(y, ty, "y"), cp, cb, wp, wb, _stream())
+    _check(st, "mdh_selective_scan")
+    return y
+
+
+def mdh_selective_scan_backward(x, dt, A, b, c, d_y, d_x, d_dt, d_A, d_b, d_c, checkpoints, skip=None, gate=None, dt_bias=None,
+                                softplus: bool = False, lengths=None, d_final_state=None, d_skip=None, d_gate=None, d_dt_bias=None,
+                                d_initial_state=None, workspace=None):
+    """Gradients of mdh_selective_scan, from the checkpoints that it left; d_A, d_skip, d_dt_bias: float32, or None."""
+    L = _lib or lib()
+    B, T = lead = x.shape[:2]
+    D, N, G = _scan_operands(lead, x, A, b, c, dt, (gate, "gate"), (d_y, "d_y"), (d_x, "d_x"), (d_dt, "d_dt"), (d_gate, "d_gate"))
+    _same(b.shape, (d_b, "d_b"), (d_c, "d_c"))
+    if (gate is None) != (d_gate is None):
+        raise ValueError("d_gate goes with gate")
+    ty = x.dtype
+    d = _dtype_of(ty)
+    (dso, dsi), _, _ = _pools(B, (D, N), _F32, None, (d_final_state, "d_final_state"), (d_initial_state, "d_initial_state"))
+    (cp, cb), (wp, wb) = _ws(checkpoints), _ws(workspace)
+    strides = _strides((x, dt, x if gate is None else gate, d_y, d_x, d_dt, d_x if gate is None else d_gate, b, c, d_b, d_c))
+    st = L.mdh_selective_scan_backward(_q5(B, T, D, N, G), d, _strided(x, ty, "x"), _strided(dt, ty, "dt"), _sp(gate, ty, "gate"),
+                                       _strided(b, ty, "b"), _strided(c, ty, "c"), _strided(d_y, ty, "d_y"), strides, _opt(A, _F32, "A"),
+                                       _opt(skip, _F32, "skip", (D,)), _opt(dt_bias, _F32, "dt_bias", (D,)), int(softplus),
+                                       _opt(lengths, _I32, "lengths", (B,)), dso, cp, cb, _strided(d_x, ty, "d_x"),
+                                       _strided(d_dt, ty, "d_dt"), _sp(d_gate, ty, "d_gate"), _strided(d_b, ty, "d_b"),
+                                       _strided(d_c, ty, "d_c"), _opt(d_A, _F32, "d_A", (D, N)), _opt(d_skip, _F32, "d_skip", (D,)),
+                                       _opt(d_dt_bias, _F32, "d_dt_bias", (D,)), dsi, wp, wb, _stream())
+    _check(st, "mdh_selective_scan_backward")
+    return d_x
+
+
+def mdh_selective_scan_step(x, dt, A, b, c, state, y, skip=None, gate=None, dt_bias=None, softplus: bool = False, slots=None):
+    """One token with the state in place.  x, dt, gate, y: (B, D); b, c: (B, G, N); state: (B, D, N) float32, or with slots (B,) int32
+    a pool (n, D, N)."""
+    L = _lib or lib()
+    B = x.shape[0]
+    D, N, G = _scan_operands((B,), x, A, b, c, dt, (y, "y"), (gate, "gate"))
+    ty = x.dtype
+    d = _dtype_of(ty)
+    (sp,), n, slots_p = _pools(B, (D, N), _F32, slots, (state, "state"))
+    st = L.mdh_selective_scan_step(_q4(B, D, N, G), d, _strided(x, ty, "x"), _strided(dt, ty, "dt"), _sp(gate, ty, "gate"),
+                                   _strided(b, ty, "b"), _strided(c, ty, "c"), _strides((x, dt, x if gate is None else gate, y, b, c)),
+                                   _opt(A, _F32, "A"), _opt(skip, _F32, "skip", (D,)), _opt(dt_bias, _F32, "dt_bias", (D,)), int(softplus),
+                                   sp, slots_p, n, _strided(y, ty, "y"), _stream())
+    _check(st, "mdh_selective_scan_step")
+    return y
+
+
+def _norm_rows(x):
+    shape = x.shape
+    if len(shape) < 2:
+        raise ValueError("x has shape %s: rows of channels are required, one row too is (1, C)" % (tuple(shape),))
+    return shape, math.prod(shape[:-1]), shape[-1]
+
+
+def mdh_layer_norm(x, weight, bias, y, eps: float = 1e-5, residual=None, total=None, mean=None, rstd=None):
+    """y = layer norm of x, or of total = x + residual (rounded to x's type), over the last dimension.  x, residual, total, y: (..., C),
+    rows evenly spaced; weight, bias: (C,) float32 or None; mean, rstd: (...) float32 or None, what the backward call wants."""
+    L = _lib or lib()
+    shape, rows, C = _norm_rows(x)
+    dt = x.dtype
+    d = _dtype_of(dt)
+    if (residual is None) != (total is None):
+        raise ValueError("total goes with residual")
+    named = ((x, "x"), (residual, "residual"), (total, "total"), (y, "y"))
+    (xp, xs), (rp, rs), (tp, ts), (yp, ys) = (_rows(t, name, shape, dt) for t, name in named)
+    strides = None if xs == ys == C and (rp is None or rs == ts == C) else struct.pack("4q", xs, rs, ts, ys)
+    st = L.mdh_layer_norm(_q2(rows, C), d, xp, rp, strides, _opt(weight, _F32, "weight", (C,)), _opt(bias, _F32, "bias", (C,)), eps, tp, yp,
+                          _opt(mean, _F32, "mean", shape[:-1]), _opt(rstd, _F32, "rstd", shape[:-1]), _stream())
+    _check(st, "mdh_layer_norm")
+    return y
+
+
+def mdh_layer_norm_workspace_size(sizes: Sequence[int], dtype) -> int:
+    """Of the backward call.  ``sizes``: (rows, C); ``dtype``: torch.float32 or torch.bfloat16."""
+    return int(lib().mdh_layer_norm_workspace_size(_q2(*sizes), _dtype_of(dtype)))
+
+
+def mdh_layer_norm_backward(x, weight, mean, rstd, d_y, d_x, d_weight, d_bias, d_total=None, workspace=None):
+    """Gradients of mdh_layer_norm.  x: what was normalised (total, where there is a residual); d_total: the gradient of total from
+    elsewhere; d_x: of x and of the residual; d_weight, d_bias: (C,) float32 or None."""
+    L = _lib or lib()
+    shape, rows, C = _norm_rows(x)
+    dt = x.dtype
+    d = _dtype_of(dt)
+    named = ((x, "x"), (d_y, "d_y"), (d_total, "d_total"), (d_x, "d_x"))
+    (xp, xs), (yp, ys), (tp, ts), (dp, ds) = (_rows(t, name, shape, dt) for t, name in named)
+    wp, wb = _ws(workspace)
+    st = L.mdh_layer_norm_backward(_q2(rows, C), d, xp, yp, tp, struct.pack("4q", xs, ys, ts, ds), _opt(weight, _F32, "weight", (C,)),
+                                   _opt(mean, _F32, "mean", shape[:-1]), _opt(rstd, _F32, "rstd", shape[:-1]), dp,
+                                   _opt(d_weight, _F32, "d_weight", (C,)), _opt(d_bias, _F32, "d_bias", (C,)), wp, wb, _stream())
+    _check(st, "mdh_layer_norm_backward")
     return d_x
 
 

@@ -40,6 +40,12 @@ SOURCES = [
     "mdh_linattn.hip",
     "mdh_linattn_step.hip",
     "mdh_group_norm.hip",
+    "mdh_api_block.hip",
+    "mdh_causal_conv.hip",
+    "mdh_selective_scan.hip",
+    "mdh_selective_scan_grad.hip",
+    "mdh_layer_norm.hip",
+    "mdh_sum_rows.hip",
 ]
 
 # packed-fp32 VALU instructions (v_pk_*_f32) are switched off on purpose: some of their forms have

@@ -352,6 +352,82 @@ size_t group_norm_workspace(const GroupNormCall& c, bool backward);
 mdh_status launch_group_norm(const GroupNormCall& c, hipStream_t st);
 mdh_status launch_group_norm_backward(const GroupNormCall& c, hipStream_t st);
 
+// ---- a selective state space block: short convolution, scan, layer norm (mdh_causal_conv.hip, mdh_selective_*, mdh_layer_norm.hip) ----
+
+// Index functions (b, t, channel) -> p[b * sb + t * st + channel] and (b, t, group, state) -> p[b * sb + t * st + g * sg + state]
+struct TokenView {
+  const void* p;
+  int64_t sb, st;
+};
+struct SharedView {
+  const void* p;
+  int64_t sb, st, sg;
+};
+struct ConvCall {
+  int64_t B, T;
+  int C, W, dtype, act;
+  TokenView x, y, dx;  // y: d_y in the backward call
+  const float *weight, *bias;
+  const int32_t *lengths, *slots;
+  int64_t n_slots;
+  const void* s_in;  // windows (batch or slot, W - 1, C); one token: s_out alone
+  void* s_out;
+  const void* d_out;  // gradients of the windows that went out and came in
+  void* d_in;
+  float *part, *dweight, *dbias;
+};
+size_t conv_workspace(const ConvCall& c);  // of the backward call
+mdh_status launch_conv(const ConvCall& c, hipStream_t st);
+mdh_status launch_conv_backward(const ConvCall& c, hipStream_t st);
+mdh_status launch_conv_step(const ConvCall& c, hipStream_t st);
+
+constexpr int kScanTile = 16;  // tokens from checkpoint to checkpoint
+struct ScanCall {
+  int64_t B, T, tiles;
+  int D, N, G, E, dtype, softplus;  // E = D / G
+  TokenView x, dt, gate, y;         // y: d_y in the backward call
+  SharedView b, c;
+  TokenView dx, ddt, dgate;
+  SharedView db, dc;
+  const float *A, *skip, *dt_bias;
+  const int32_t *lengths, *slots;
+  int64_t n_slots;
+  const float* s_in;  // backward: gradient of the final states; one token: s_out alone
+  float* s_out;       // backward: gradient of the initial states
+  float* checkpoints;
+  float *dA, *dskip, *ddt_bias;
+  void* ws;
+};
+size_t scan_workspace(const ScanCall& c);
+size_t scan_backward_workspace(const ScanCall& c);
+mdh_status launch_scan_forward(const ScanCall& c, hipStream_t st);
+mdh_status launch_scan_backward(const ScanCall& c, hipStream_t st);
+mdh_status launch_scan_step(const ScanCall& c, hipStream_t st);
+// h (b, n segments, D, N), what each segment leaves from zeros -> what each begins with; sum: its deltas (b, n, D)
+mdh_status launch_scan_segments(const ScanCall& c, float* h, float* sum, int n, const float* start, bool rev, hipStream_t st);
+
+struct LayerNormCall {
+  int64_t rows;
+  int C, dtype;
+  RowView x, residual, total, y;  // y: d_y in the backward call
+  RowView dtotal, dx;
+  const float *weight, *bias;
+  float eps;
+  float *mean, *rstd;
+  float *dweight, *dbias;
+  void* ws;
+};
+size_t layer_norm_workspace(const LayerNormCall& c);  // of the backward call
+mdh_status launch_layer_norm(const LayerNormCall& c, hipStream_t st);
+mdh_status launch_layer_norm_backward(const LayerNormCall& c, hipStream_t st);
+
+// columns of rows x n partial results, summed in a fixed order: the first to[0].n to to[0].p, and so on (null: not wanted)
+struct SumTarget {
+  float* p;
+  int64_t n;
+};
+mdh_status launch_sum_rows(const float* part, int64_t rows, int64_t n, const SumTarget (&to)[3], hipStream_t st);
+
 // The runtime's "last error" is sticky per thread and other users of the runtime in the same
 // process leave harmless codes there (an event query that is not ready yet, for instance):
 // clear it before a launch so that the status read after the launch is that launch's own.

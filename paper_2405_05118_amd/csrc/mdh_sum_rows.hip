@@ -1,0 +1,51 @@
+// Column sums of a matrix of fp32 partial results, in a fixed order: gradients of parameters, one row for each share of the
+// tokens.  Four teams of a workgroup take every fourth row of 64 columns, their sums are added in order.
+#include "mdh_internal.h"
+
+namespace mdh {
+namespace {
+
+constexpr int kTeams = 4;
+
+struct SumArgs {
+  const float* part;
+  int64_t rows, n;
+  SumTarget to[3];
+};
+
+__global__ __launch_bounds__(64 * kTeams) void sum_rows_kernel(SumArgs s) {
+  __shared__ float sums[kTeams][64];
+  const int lane = threadIdx.x & 63, team = threadIdx.x >> 6;
+  int64_t col = (int64_t)blockIdx.x * 64 + lane;
+  float x[4] = {0.f, 0.f, 0.f, 0.f};
+  if (col < s.n) {
+    const float* p = s.part + col;
+    int64_t r = team;
+    for (; r + 3 * kTeams < s.rows; r += 4 * kTeams)
+#pragma unroll
+      for (int u = 0; u < 4; ++u) x[u] += p[(r + u * kTeams) * s.n];
+    for (; r < s.rows; r += kTeams) x[0] += p[r * s.n];
+  }
+  sums[team][lane] = (x[0] + x[1]) + (x[2] + x[3]);
+  __syncthreads();
+  if (team || col >= s.n) return;
+  const float v = (sums[0][lane] + sums[1][lane]) + (sums[2][lane] + sums[3][lane]);
+#pragma unroll
+  for (int i = 0; i < 3; ++i) {
+    if (col >= 0 && col < s.to[i].n && s.to[i].p) s.to[i].p[col] = v;
+    col -= s.to[i].n;
+  }
+}
+
+}  // namespace
+
+mdh_status launch_sum_rows(const float* part, int64_t rows, int64_t n, const SumTarget (&to)[3], hipStream_t st) {
+  if (n == 0) return MDH_OK;
+  if (cdiv(n, 64) * 64 * kTeams >= (int64_t)1 << 32) return MDH_ERR_SIZE;
+  const SumArgs s{part, rows, n, {to[0], to[1], to[2]}};
+  clear_stale_error();
+  sum_rows_kernel<<<(unsigned)cdiv(n, 64), 64 * kTeams, 0, st>>>(s);
+  return launch_status();
+}
+
+}  // namespace mdh
