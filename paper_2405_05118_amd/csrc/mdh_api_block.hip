@@ -165,9 +165,9 @@ mdh_status mdh_selective_scan(const int64_t* sizes, mdh_dtype dtype, const void*
   if (short_of(workspace, workspace_bytes, scan_workspace(c))) return MDH_ERR_WORKSPACE;
   if (checkpoints && short_of(checkpoints, checkpoints_bytes, checkpoint_bytes(c))) return MDH_ERR_WORKSPACE;
   auto view = [&](const void* p, int i) { return tokens(p, strides ? strides + 2 * i : nullptr, c.B, c.T, c.D); };
-  c.x = view(x, 0), c.dt = view(dt, 1), c.gate = view(gate, 2), c.y = view(y, 3);
-  c.b = shared(b, strides ? strides + 8 : nullptr, c), c.c = shared(c_, strides ? strides + 11 : nullptr, c);
-  if (overlaps(c.y, c.B, c.T)) return MDH_ERR_SIZE;
+  c.in[0] = view(x, 0), c.in[1] = view(dt, 1), c.in[2] = view(gate, 2), c.out[0] = view(y, 3);
+  c.bc[0] = shared(b, strides ? strides + 8 : nullptr, c), c.bc[1] = shared(c_, strides ? strides + 11 : nullptr, c);
+  if (overlaps(c.out[0], c.B, c.T)) return MDH_ERR_SIZE;
   c.A = A, c.skip = skip, c.dt_bias = dt_bias, c.softplus = softplus != 0, c.lengths = lengths, c.slots = slots, c.n_slots = n_slots;
   c.s_in = initial_state, c.s_out = final_state, c.checkpoints = (float*)checkpoints, c.ws = workspace;
   return launch_scan_forward(c, (hipStream_t)stream);
@@ -192,12 +192,12 @@ mdh_status mdh_selective_scan_backward(const int64_t* sizes, mdh_dtype dtype, co
     return MDH_ERR_WORKSPACE;
   auto view = [&](const void* p, int i) { return tokens(p, strides ? strides + 2 * i : nullptr, c.B, c.T, c.D); };
   auto view2 = [&](const void* p, int i) { return shared(p, strides ? strides + 14 + 3 * i : nullptr, c); };
-  c.x = view(x, 0), c.dt = view(dt, 1), c.gate = view(gate, 2), c.y = view(d_y, 3);
-  c.dx = view(d_x, 4), c.ddt = view(d_dt, 5), c.dgate = view(gate ? d_gate : nullptr, 6);
-  c.b = view2(b, 0), c.c = view2(c_, 1), c.db = view2(d_b, 2), c.dc = view2(d_c, 3);
-  if (overlaps(c.dx, c.B, c.T) || overlaps(c.ddt, c.B, c.T) || (gate && overlaps(c.dgate, c.B, c.T)) || overlaps(c.db, c) ||
-      overlaps(c.dc, c))
-    return MDH_ERR_SIZE;
+  c.in[0] = view(x, 0), c.in[1] = view(dt, 1), c.in[2] = view(gate, 2), c.in[3] = view(d_y, 3);
+  c.out[0] = view(d_x, 4), c.out[1] = view(d_dt, 5), c.out[2] = view(gate ? d_gate : nullptr, 6);
+  c.bc[0] = view2(b, 0), c.bc[1] = view2(c_, 1), c.dbc[0] = view2(d_b, 2), c.dbc[1] = view2(d_c, 3);
+  for (int i = 0; i < (gate ? 3 : 2); ++i)
+    if (overlaps(c.out[i], c.B, c.T)) return MDH_ERR_SIZE;
+  if (overlaps(c.dbc[0], c) || overlaps(c.dbc[1], c)) return MDH_ERR_SIZE;
   c.A = A, c.skip = skip, c.dt_bias = dt_bias, c.softplus = softplus != 0, c.lengths = lengths;
   c.s_in = d_final_state, c.s_out = d_initial_state, c.checkpoints = (float*)checkpoints, c.ws = workspace;
   c.dA = d_A, c.dskip = d_skip, c.ddt_bias = d_dt_bias;
@@ -223,9 +223,9 @@ mdh_status mdh_selective_scan_step(const int64_t* sizes, mdh_dtype dtype, const 
     const int64_t s[3] = {strides ? strides[4 + 2 * i] : (int64_t)c.G * c.N, 0, strides ? strides[5 + 2 * i] : c.N};
     return shared(p, s, c);
   };
-  c.x = view(x, 0), c.dt = view(dt, 1), c.gate = view(gate, 2), c.y = view(y, 3);
-  c.b = view2(b, 0), c.c = view2(c_, 1);
-  if (overlaps(c.y, c.B, 1)) return MDH_ERR_SIZE;
+  c.in[0] = view(x, 0), c.in[1] = view(dt, 1), c.in[2] = view(gate, 2), c.out[0] = view(y, 3);
+  c.bc[0] = view2(b, 0), c.bc[1] = view2(c_, 1);
+  if (overlaps(c.out[0], c.B, 1)) return MDH_ERR_SIZE;
   c.A = A, c.skip = skip, c.dt_bias = dt_bias, c.softplus = softplus != 0, c.slots = slots, c.n_slots = n_slots, c.s_out = state;
   return launch_scan_step(c, (hipStream_t)stream);
 }

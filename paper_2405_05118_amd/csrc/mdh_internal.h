@@ -385,10 +385,9 @@ constexpr int kScanTile = 16;  // tokens from checkpoint to checkpoint
 struct ScanCall {
   int64_t B, T, tiles;
   int D, N, G, E, dtype, softplus;  // E = D / G
-  TokenView x, dt, gate, y;         // y: d_y in the backward call
-  SharedView b, c;
-  TokenView dx, ddt, dgate;
-  SharedView db, dc;
+  TokenView in[4];                  // x, dt, gate (null: none), d_y of the backward call
+  TokenView out[3];                 // y; backward: d_x, d_dt, d_gate
+  SharedView bc[2], dbc[2];         // b, c and their gradients
   const float *A, *skip, *dt_bias;
   const int32_t *lengths, *slots;
   int64_t n_slots;

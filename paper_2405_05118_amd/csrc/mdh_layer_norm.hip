@@ -1,8 +1,9 @@
 // Layer norm of rows, with the sum that a residual stream takes in front of it: s = x + residual, y = (s - mean) rstd w + b.
 // A few operations a value: bound by memory, or by a launch.
 //
-// A row is read once: L lanes (8 to 1024) hold it, P pieces of 16 bytes each, and exchange two sums.  The mean is put right by
-// the sum of the differences from it: the variance of equal values is 0 whatever the mean was rounded to.  Wider rows than
+// A row is read once: L lanes (8 to 1024) hold it, P pieces of 16 bytes each, and exchange two sums.  Where the mean
+// is large against the spread it is put right by the sum of the differences: equal values have that value as their mean and the
+// variance 0 whatever their sum was rounded to.  Wider rows than
 // 16384 are read again for every sum.  In the backward call a workgroup keeps its columns and walks the rows, its share of the
 // gradients of weight and bias in registers; one row of the workspace for each workgroup, added up in order by a second launch.
 #include "mdh_internal.h"
@@ -49,8 +50,10 @@ __device__ __forceinline__ Moments moments(float sum, int C, float eps, int& tur
   differ(mean, d, d2);
   row_sums<L>(d, d2, turn);
   const float off = d * over, var = fmaxf(d2 * over - off * off, 0.f);
+  // (means within 16 times the spread are right as they are: the differences' own roundings would be added to them)
+  if (mean * mean > 256.f * var) mean += off;
   // NaN and infinity stay: fmaxf would drop NaN
-  return Moments{mean + off, 1.f / sqrtf((d2 == d2 ? var : d2) + eps)};
+  return Moments{mean, 1.f / sqrtf((d2 == d2 ? var : d2) + eps)};
 }
 
 template <typename T, int L, int P>

@@ -4,7 +4,7 @@
 
 #include "mdh_act.h"
 #include "mdh_internal.h"
-#include "mdh_types.h"
+#include "mdh_vec.h"
 
 namespace mdh {
 
@@ -27,6 +27,12 @@ template <int J>
 __device__ __forceinline__ float lane_of_row(float v) {
   return __int_as_float(__builtin_amdgcn_mov_dpp(__float_as_int(v), 0x150 + J, 0xf, 0xf, true));
 }
+// The same value to be broadcast at another place: where the compiler knows that two broadcasts are one, it keeps their result in
+// a register of its own, 16 for a tile, and both lose the modifier.
+__device__ __forceinline__ float again(float v) {
+  asm("" : "+v"(v));
+  return v;
+}
 // 2^x by the hardware (1 ulp; 0 below 2^-126)
 __device__ __forceinline__ float exp2_of(float x) { return __builtin_amdgcn_exp2f(x); }
 
@@ -39,20 +45,20 @@ __device__ __forceinline__ float exp_of(float v) {
 // log(1 + e^v).  log(1 + e) = 2 artanh(e / (2 + e)), whose series of five terms is off by less than 2^-26 up to e = 0.4
 // (s = 1/6: s^10 / 11); beyond, 1 + e is rounded by 2^-24 of a logarithm above 0.33.
 __device__ __forceinline__ float softplus_of(float v) {
-  if (v > 20.f) return v;  // e^-20 is below half an ulp of 20
   const float e = exp_of(v);
   const float s = e * __builtin_amdgcn_rcpf(2.f + e), q = s * s;
   const float near = 2.f * s * fmaf(q, fmaf(q, fmaf(q, fmaf(q, 1.f / 9, 1.f / 7), 1.f / 5), 1.f / 3), 1.f);
-  return e <= 0.4f ? near : kLn2 * __builtin_amdgcn_logf(1.f + e);
+  const float far = kLn2 * __builtin_amdgcn_logf(1.f + e), both = e <= 0.4f ? near : far;
+  return v > 20.f ? v : both;  // (e^-20 is below half an ulp of 20; NaN stays)
 }
 
 struct ScanPlace {
-  int64_t b, seg, len, first, last;  // tiles first <= t < last, those of them before the length
-  int g, block;                      // group, block of its channels
-  int row, j;                        // the lane: row of its workgroup, place in the row
+  int64_t b, len;
+  int64_t first, last, alive;  // tokens of the segment; up to its last valid one
+  int seg, g, block;           // block: of the group's channels
+  int row, j;                  // the lane: row of its workgroup, place in the row
 };
 
-// channels of a workgroup of `waves` wavefronts, walked `times` channels a row
 __device__ __forceinline__ int64_t scan_length(const ScanCall& c, int64_t b) {
   return c.lengths ? min(max((int64_t)c.lengths[b], (int64_t)0), c.T) : c.T;
 }
@@ -62,17 +68,17 @@ __device__ __forceinline__ int64_t scan_slot(const ScanCall& c, int64_t b) {
   return s >= 0 && s < c.n_slots ? s : -1;
 }
 // workgroup id -> (batch, segment, group, block), blocks fastest (neighbours read the same lines: xcd_order)
-__device__ __forceinline__ ScanPlace scan_place(const ScanCall& c, int blocks, int nseg, int64_t seg_tiles) {
+__device__ __forceinline__ ScanPlace scan_place(const ScanCall& c, int blocks, int nseg, int64_t seg_tokens) {
   ScanPlace p;
-  int64_t i = xcd_order(blockIdx.x, gridDim.x);
-  p.block = (int)(i % blocks), i /= blocks;
-  p.g = (int)(i % c.G), i /= c.G;
-  p.seg = i % nseg;
-  p.b = i / nseg;
+  unsigned i = xcd_order(blockIdx.x, gridDim.x);
+  p.block = (int)(i % (unsigned)blocks), i /= (unsigned)blocks;
+  p.g = (int)(i % (unsigned)c.G), i /= (unsigned)c.G;
+  p.seg = (int)(i % (unsigned)nseg);
+  p.b = i / (unsigned)nseg;
   p.len = scan_length(c, p.b);
-  const int64_t tiles = (c.T + kTile - 1) / kTile;
-  p.first = p.seg * seg_tiles;
-  p.last = min(p.first + seg_tiles, tiles);
+  p.first = p.seg * seg_tokens;
+  p.last = min(p.first + seg_tokens, c.T);
+  p.alive = min(p.last, p.len);
   p.j = threadIdx.x & 15;
   p.row = threadIdx.x >> 4;
   return p;
@@ -86,25 +92,144 @@ __device__ __forceinline__ T* at(const SharedView& v, int64_t b, int64_t t, int 
   return (T*)const_cast<void*>(v.p) + b * v.sb + t * v.st + g * v.sg + n;
 }
 
-// b or c of a tile in LDS as fp32, state by state with kTile tokens each; zeros past the length and past N.
-constexpr int kPitch = kTile + 4;  // (16 lanes that read 16 bytes each: all 64 banks)
-template <typename T, int STATES, int THREADS>
-__device__ __forceinline__ void stage_shared(const ScanCall& c, const SharedView& v, const ScanPlace& p, int64_t t0, float* lds) {
+// Tokens are staged in LDS in blocks: the loads of the next block are under way while one is worked on.  All operands of a block are
+// one list of pieces of 16 bytes, dealt out to the lanes of the workgroup (read element by element, the 16 tokens of a tile cost the
+// caches an access for each token and wavefront, 1.4e8 for 8192 tokens of 4096 channels: one a cycle, as much as all the rest;
+// operand by operand, most of the lanes had nothing to do).
+//   token operands   (x, dt, ..) CH channels, in LDS as they are in memory: piece q at raw + q; gradients and outputs take the places
+//                    of the first ones, and a lane stores the pieces that it stages
+//   shared operands  (b, c) in LDS as fp32, state by state
+// Zeros from the end of the valid tokens on, and past the last channel or state.  The pieces of a token are exchanged so that a
+// channel's 16 tokens lie in different banks.
+template <int PA>
+__device__ __forceinline__ int swizzle(int q) {
+  const int t = q / PA;
+  return q ^ (t / (16 / PA) & (PA - 1));
+}
+// where channel ch of token t of a block of CH channels is
+template <typename T, int CH>
+__device__ __forceinline__ int place_of(int t, int ch) {
+  constexpr int V = kLaneValues<T>, PA = CH / V;
+  return swizzle<PA>(t * PA + ch / V) * V + ch % V;
+}
+template <typename T, int NA, int NB, int CH, int STATES, int TOKENS, int THREADS>
+struct Stage {
+  static constexpr int V = kLaneValues<T>, PA = CH / V, QA = TOKENS * PA, PB = STATES / V, QB = TOKENS * PB;
+  static constexpr int PIECES = NA * QA + NB * QB, SLOTS = (PIECES + THREADS - 1) / THREADS;
+  static constexpr int kPitch = TOKENS + 4, kFloats = STATES * kPitch;  // (16 lanes that read 16 bytes each reach all 64 banks)
+  static_assert(QA % 64 == 0 && QB % 64 == 0 && THREADS % 64 == 0, "a wavefront's pieces are of one operand");
+  Word4 w[SLOTS];
+  const T* at[SLOTS];   // of the block that is loaded next
+  int64_t step[SLOTS];  // to the one after it
+  int left[SLOTS];      // channels or states from there on
+
+  // which operand a wavefront's pieces are of (PIECES / .. and on: none)
+  __device__ __forceinline__ static int operand(int k) {
+    const int q = __builtin_amdgcn_readfirstlane(k * THREADS + (int)threadIdx.x);
+    return q < NA * QA ? q / QA : NA + (q - NA * QA) / QB;
+  }
+  __device__ __forceinline__ static int token(int k) {
+    const int q = k * THREADS + (int)threadIdx.x;
+    return operand(k) < NA ? q % QA / PA : (q - NA * QA) % QB / PB;
+  }
+  // token operands that are not there have null pointers
+  // way: 1 from the first block to the last, -1 back
+  __device__ __forceinline__ void begin(const TokenView* va, const SharedView* vb, const ScanPlace& p, int64_t t0, int way, int64_t d0, int width,
+                                        int N) {
 #pragma unroll
-  for (int i0 = 0; i0 < STATES * kTile; i0 += THREADS) {
-    const int i = i0 + threadIdx.x, n = i % STATES, t = i / STATES;
-    if (i < STATES * kTile) lds[n * kPitch + t] = n < c.N && t0 + t < p.len ? to_float(*at<T>(v, p.b, t0 + t, p.g, n)) : 0.f;
+    for (int k = 0; k < SLOTS; ++k) {
+      const int o = operand(k), q = k * THREADS + (int)threadIdx.x;
+      at[k] = nullptr, step[k] = 0, left[k] = 0;
+      if (o < NA) {
+        const int ch = q % QA % PA * V;
+        at[k] = (const T*)va[o].p + p.b * va[o].sb + (t0 + token(k)) * va[o].st + d0 + ch;
+        step[k] = way * TOKENS * va[o].st;
+        left[k] = va[o].p ? width - ch : 0;
+      } else if (o < NA + NB) {
+        const int n = (q - NA * QA) % QB % PB * V;
+        const SharedView& v = vb[o - NA];
+        at[k] = (const T*)v.p + p.b * v.sb + (t0 + token(k)) * v.st + p.g * v.sg + n;
+        step[k] = way * TOKENS * v.st;
+        left[k] = N - n;
+      }
+    }
+  }
+  // `tokens` valid ones of the block; then on to the next one
+  __device__ __forceinline__ void load(int64_t tokens) {
+    const int valid = (int)min(tokens, (int64_t)TOKENS);
+#pragma unroll
+    for (int k = 0; k < SLOTS; ++k) {
+      w[k] = (Word4){0, 0, 0, 0};
+      if (left[k] > 0 && token(k) < valid) w[k] = load_row<T>(at[k], left[k]);
+      at[k] += step[k];
+    }
+  }
+  __device__ __forceinline__ void stage(T* raw, float* shared) const {
+#pragma unroll
+    for (int k = 0; k < SLOTS; ++k) {
+      const int o = operand(k), q = k * THREADS + (int)threadIdx.x;
+      if (o < NA) {
+        ((Word4*)raw)[q / QA * QA + swizzle<PA>(q % QA)] = w[k];
+      } else if (o < NA + NB) {
+        float x[V];
+        unpack_row<T>(w[k], x);
+        float* to = shared + (o - NA) * kFloats + (q - NA * QA) % QB % PB * V * kPitch + token(k);
+#pragma unroll
+        for (int i = 0; i < V; ++i) to[i * kPitch] = x[i];
+      }
+    }
+  }
+};
+
+// Outputs of a block, NO of them, in the places of the first token operands of a Stage
+template <typename T, int NO, int CH, int TOKENS, int THREADS>
+struct Outputs {
+  static constexpr int V = kLaneValues<T>, PA = CH / V, QA = TOKENS * PA, SLOTS = (NO * QA + THREADS - 1) / THREADS;
+  Word4 w[SLOTS];
+  T* at[SLOTS];
+  int64_t step[SLOTS];
+  int left[SLOTS];
+  __device__ __forceinline__ static int operand(int k) { return __builtin_amdgcn_readfirstlane(k * THREADS + (int)threadIdx.x) / QA; }
+  __device__ __forceinline__ void begin(const TokenView* to, const ScanPlace& p, int64_t t0, int way, int64_t d0, int width) {
+#pragma unroll
+    for (int k = 0; k < SLOTS; ++k) {
+      const int o = operand(k), q = (k * THREADS + (int)threadIdx.x) % QA, ch = q % PA * V;
+      at[k] = nullptr, step[k] = 0, left[k] = 0;
+      if (o < NO && to[o].p) {
+        at[k] = (T*)const_cast<void*>(to[o].p) + p.b * to[o].sb + (t0 + q / PA) * to[o].st + d0 + ch;
+        step[k] = way * TOKENS * to[o].st;
+        left[k] = width - ch;
+      }
+    }
+  }
+  __device__ __forceinline__ void take(const T* raw) {
+#pragma unroll
+    for (int k = 0; k < SLOTS; ++k) {
+      const int q = k * THREADS + (int)threadIdx.x;
+      if (NO * QA % THREADS == 0 || q < NO * QA) w[k] = ((const Word4*)raw)[q / QA * QA + swizzle<PA>(q % QA)];
+    }
+  }
+  // `tokens` of the block are the segment's; then on to the next one
+  __device__ __forceinline__ void store(int64_t tokens) {
+    const int valid = (int)min(tokens, (int64_t)TOKENS);
+#pragma unroll
+    for (int k = 0; k < SLOTS; ++k) {
+      if (left[k] > 0 && (k * THREADS + (int)threadIdx.x) % QA / PA < valid) store_row<T>(at[k], left[k], w[k]);
+      at[k] += step[k];
+    }
+  }
+};
+// zeros behind the block of tokens that the length is in
+template <typename T, int CH, int THREADS>
+__device__ __forceinline__ void store_zeros(const TokenView& v, const ScanPlace& p, int64_t d0, int width, int block) {
+  constexpr int V = kLaneValues<T>, P = CH / V;
+  const int64_t from = p.alive > p.first ? p.first + (p.alive - p.first + block - 1) / block * block : p.first;
+  for (int64_t t = from + (int)threadIdx.x / P; t < p.last; t += THREADS / P) {
+    const int ch = (int)threadIdx.x % P * V;
+    if (ch < width) store_row<T>((T*)const_cast<void*>(v.p) + p.b * v.sb + t * v.st + d0 + ch, width - ch, (Word4){0, 0, 0, 0});
   }
 }
-__device__ __forceinline__ void tile_of(const float* lds, int n, float (&x)[kTile]) {
-  typedef float f4 __attribute__((ext_vector_type(4)));
-#pragma unroll
-  for (int i = 0; i < kTile / 4; ++i) {
-    const f4 v = ((const f4*)(lds + n * kPitch))[i];
-#pragma unroll
-    for (int e = 0; e < 4; ++e) x[4 * i + e] = v[e];
-  }
-}
+__device__ __forceinline__ Float4 four_of(const float* lds) { return *(const Float4*)lds; }
 
 // Sums over the 16 lanes of a row, for 16 tokens at once: every lane leaves its value for token t at t * 68 + lane and lane j
 // adds up token j's (68: 16 lanes that read 16 bytes each reach all 64 banks).  A wavefront's own part of LDS, in order.
@@ -114,6 +239,14 @@ __device__ __forceinline__ float row_sum(const float* lds, int lane) {
   const f4* p = (const f4*)(lds + (lane & 15) * kSumPitch + (lane & 48));
   const f4 s = (p[0] + p[1]) + (p[2] + p[3]);
   return (s[0] + s[1]) + (s[2] + s[3]);
+}
+// The same values summed over the four rows of a wavefront: lane (r, j) those of lanes j for tokens 4 r + 0 .. 3
+__device__ __forceinline__ Float4 over_rows(const float* lds, int lane) {
+  const float* p = lds + (lane >> 4) * 4 * kSumPitch + (lane & 15);
+  Float4 s;
+#pragma unroll
+  for (int i = 0; i < 4; ++i) s[i] = (p[i * kSumPitch] + p[i * kSumPitch + 16]) + (p[i * kSumPitch + 32] + p[i * kSumPitch + 48]);
+  return s;
 }
 // between a wavefront's stores to LDS and other lanes' loads of them, and back
 __device__ __forceinline__ void wave_fence() {
@@ -125,13 +258,12 @@ __device__ __forceinline__ void wave_fence() {
 struct Token {
   float x, delta, raw;  // raw: before the softplus
 };
-template <typename T>
-__device__ __forceinline__ Token token_of(const ScanCall& c, bool live, const T* x, const T* dt, float dt_bias) {
-  Token k{0.f, 0.f, 0.f};
-  if (!live) return k;
-  k.x = to_float(*x);
-  k.raw = to_float(*dt) + dt_bias;
-  k.delta = c.softplus ? softplus_of(k.raw) : k.raw;
+__device__ __forceinline__ Token token_of(const ScanCall& c, float x, float dt, bool live, float dt_bias) {
+  Token k;
+  k.x = x;
+  k.raw = dt + dt_bias;
+  const float delta = c.softplus ? softplus_of(k.raw) : k.raw;
+  k.delta = live ? delta : 0.f;
   return k;
 }
 

@@ -15,25 +15,48 @@
 namespace mdh {
 namespace {
 
-constexpr int kThreads = 256, kChannels = kThreads / 16;
-
 // what the segments leave: h of (b, seg, d, n) and the sum of deltas of (b, seg, d)
 struct Segments {
   float *h, *sum;
   int n;
-  int64_t tiles;  // of one
+  int64_t tokens;  // of one
 };
 
+// A workgroup has CH channels, and W tiles of tokens at once (W = 1: one after the other).  Tiles at once: every wavefront walks its own
+// from a state of zeros, keeping h and the product of the factors for every token; the tiles' ends meet in LDS, and h + product *
+// (state before the tile) is what the walk from there would give: 6 multiplications a step for which no token is walked twice.
+template <int NS, int CH_, int W_, int TOKENS_>
+struct Form {
+  static constexpr int CH = CH_, W = W_, TOKENS = TOKENS_, THREADS = 16 * CH * W;
+  static_assert(W == 1 || TOKENS == W * kTile, "a wavefront has one tile of a block");
+};
+template <int NS>
+using InTurn = Form<NS, 16, 1, NS == 4 ? 32 : 64>;
+template <int NS>
+using AtOnce = Form<NS, 8, 4, 64>;
+template <int NS>
+using ManyAtOnce = Form<NS, 8, 8, 128>;
+
 // STATES_ONLY: a segment's own state and sum of deltas.  Else the pass.
-template <typename T, int NS, bool STATES_ONLY>
-__global__ __launch_bounds__(kThreads) void scan_kernel(ScanCall c, Segments segs, int blocks) {
-  constexpr int S = NS * 16;
-  __shared__ float bs[S * kPitch], cs[STATES_ONLY ? 1 : S * kPitch], sums[STATES_ONLY ? 1 : kThreads / 64][kSumFloats];
-  const ScanPlace p = scan_place(c, blocks, segs.n, segs.tiles);
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-  const int e = p.block * kChannels + p.row;
-  const bool mine = e < c.E;
-  const int64_t d = (int64_t)p.g * c.E + e, slot = scan_slot(c, p.b);
+template <typename T, int NS, typename F, bool STATES_ONLY>
+__global__ __launch_bounds__(F::THREADS) void scan_kernel(ScanCall c, Segments segs, int blocks) {
+  constexpr int S = NS * 16, CH = F::CH, W = F::W, TOKENS = F::TOKENS, NA = STATES_ONLY ? 2 : 3, NB = STATES_ONLY ? 1 : 2;
+  typedef Stage<T, NA, NB, CH, S, TOKENS, F::THREADS> In;
+  typedef Outputs<T, 1, CH, TOKENS, F::THREADS> Out;
+  __shared__ T raw[NA * TOKENS * CH] __attribute__((aligned(16)));
+  __shared__ float bc[NB * In::kFloats] __attribute__((aligned(16)));
+  __shared__ float sums[STATES_ONLY ? 1 : F::THREADS / 64][STATES_ONLY ? 4 : kSumFloats] __attribute__((aligned(16)));
+  __shared__ float2 ends[W > 1 ? W : 1][W > 1 ? CH * S : 1];
+  T *const xs = raw, *const dts = raw + TOKENS * CH, *const gates = raw + 2 * TOKENS * CH;
+  ScanPlace p = scan_place(c, blocks, segs.n, segs.tokens);
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, tile = p.row / CH;
+  p.row %= CH;
+  const int e0 = p.block * CH, width = min(CH, c.E - e0);
+  const bool mine = p.row < width;
+  const int64_t d0 = (int64_t)p.g * c.E + e0, d = d0 + p.row, slot = scan_slot(c, p.b);
+  In in;
+  in.begin(c.in, c.bc, p, p.first, 1, d0, width, c.N);
+  if (p.first < p.alive) in.load(p.alive - p.first);
   float A[NS], h[NS], skip = 0.f, dt_bias = 0.f, total = 0.f;
   const int64_t seg_state = ((p.b * segs.n + p.seg) * c.D + d) * c.N;
 #pragma unroll
@@ -53,49 +76,110 @@ __global__ __launch_bounds__(kThreads) void scan_kernel(ScanCall c, Segments seg
     skip = c.skip ? c.skip[d] : 0.f;
     dt_bias = c.dt_bias ? c.dt_bias[d] : 0.f;
   }
-  for (int64_t tile = p.first; tile < p.last; ++tile) {
-    const int64_t t0 = tile * kTile, t = t0 + p.j;
-    if (t0 >= p.len) {  // nothing is left of the sequence
-      if (!STATES_ONLY && mine && t < c.T) *at<T>(c.y, p.b, t, d) = from_float<T>(0.f);
-      continue;
-    }
-    if (!STATES_ONLY && c.checkpoints)
+  auto keep = [&](int64_t t, const float (&state)[NS]) {
+    if (STATES_ONLY || !c.checkpoints || t >= p.alive) return;
 #pragma unroll
-      for (int s = 0; s < NS; ++s)
-        if (mine && s * 16 + p.j < c.N) c.checkpoints[((p.b * c.tiles + tile) * c.D + d) * c.N + s * 16 + p.j] = h[s];
-    const bool live = mine && t < p.len;
-    const Token k = token_of<T>(c, live, at<T>(c.x, p.b, t, d), at<T>(c.dt, p.b, t, d), dt_bias);
-    const float gate = !STATES_ONLY && c.gate.p && live ? to_float(*at<T>(c.gate, p.b, t, d)) : 0.f;
-    const float in = k.delta * k.x;
-    total += k.delta;
+    for (int s = 0; s < NS; ++s)
+      if (mine && s * 16 + p.j < c.N) c.checkpoints[((p.b * c.tiles + t / kTile) * c.D + d) * c.N + s * 16 + p.j] = state[s];
+  };
+  Out out;
+  if (!STATES_ONLY) out.begin(c.out, p, p.first, 1, d0, width);
+  for (int64_t t0 = p.first; t0 < p.alive; t0 += TOKENS) {
+    if (!STATES_ONLY && t0 > p.first) out.take(raw);
+    in.stage(raw, bc);
     __syncthreads();
-    stage_shared<T, S, kThreads>(c, c.b, p, t0, bs);
-    if (!STATES_ONLY) stage_shared<T, S, kThreads>(c, c.c, p, t0, cs);
+    // (stores go out behind the wait for the block's loads: what is waited for next has been under way for long)
+    if (!STATES_ONLY && t0 > p.first) out.store(TOKENS);
+    if (t0 + TOKENS < p.alive) in.load(p.alive - t0 - TOKENS);
+    const int tokens = (int)min((int64_t)TOKENS, p.alive - t0);
+    for (int i0 = tile * kTile; i0 < (W > 1 ? (tile + 1) * kTile : tokens); i0 += kTile) {
+      const int at = place_of<T, CH>(i0 + p.j, p.row);
+      const bool live = i0 + p.j < tokens;
+      const Token k = token_of(c, to_float(xs[at]), to_float(dts[at]), live, dt_bias);
+      const float u = k.delta * k.x;
+      total += k.delta;
+      float y[kTile];
+      const float* bs = bc + p.j * In::kPitch + i0;
+      if constexpr (W == 1) {
+        keep(t0 + i0, h);
+#pragma unroll
+        for (int s = 0; s < NS; ++s)
+          unroll<kTile / 4>([&](auto quarter) {
+            constexpr int Q = decltype(quarter)::value * 4;
+            const Float4 bt = four_of(bs + s * 16 * In::kPitch + Q), ct = four_of(bs + (STATES_ONLY ? 0 : In::kFloats) + s * 16 * In::kPitch + Q);
+            unroll<4>([&](auto i) {
+              constexpr int I = decltype(i)::value;
+              const float a = exp2_of(lane_of_row<Q + I>(k.delta) * A[s]);
+              h[s] = fmaf(a, h[s], lane_of_row<Q + I>(u) * bt[I]);
+              if (!STATES_ONLY) y[Q + I] = s ? fmaf(ct[I], h[s], y[Q + I]) : ct[I] * h[s];
+            });
+          });
+      } else {
+        float own[NS][kTile], product[NS][kTile];
+#pragma unroll
+        for (int s = 0; s < NS; ++s) {
+          float from_zero = 0.f, all = 1.f;
+          unroll<kTile / 4>([&](auto quarter) {
+            constexpr int Q = decltype(quarter)::value * 4;
+            const Float4 bt = four_of(bs + s * 16 * In::kPitch + Q);
+            unroll<4>([&](auto i) {
+              constexpr int I = decltype(i)::value;
+              const float a = exp2_of(lane_of_row<Q + I>(k.delta) * A[s]);
+              from_zero = fmaf(a, from_zero, lane_of_row<Q + I>(u) * bt[I]);
+              all *= a;
+              own[s][Q + I] = from_zero, product[s][Q + I] = all;
+            });
+          });
+          ends[tile][(s * CH + p.row) * 16 + p.j] = make_float2(from_zero, all);
+        }
+        __syncthreads();
+        float before[NS];
+#pragma unroll
+        for (int s = 0; s < NS; ++s) {
+          before[s] = h[s];
+#pragma unroll
+          for (int v = 0; v < W; ++v) {
+            const float2 end = ends[v][(s * CH + p.row) * 16 + p.j];
+            if (v == tile) before[s] = h[s];
+            h[s] = fmaf(end.y, h[s], end.x);
+          }
+        }
+        keep(t0 + i0, before);
+#pragma unroll
+        for (int s = 0; s < NS; ++s)
+#pragma unroll
+          for (int q = 0; q < kTile; q += 4) {
+            const Float4 ct = four_of(bs + In::kFloats + s * 16 * In::kPitch + q);
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+              const float v = fmaf(product[s][q + i], before[s], own[s][q + i]);
+              y[q + i] = s ? fmaf(ct[i], v, y[q + i]) : ct[i] * v;
+            }
+          }
+      }
+      if (!STATES_ONLY) {
+        wave_fence();
+#pragma unroll
+        for (int i = 0; i < kTile; ++i) sums[wave][i * kSumPitch + lane] = y[i];
+        wave_fence();
+        float v = row_sum(sums[wave], lane) + skip * k.x;
+        if (c.in[2].p) {
+          const float g = to_float(gates[at]);
+          v *= g * sigmoid(g);
+        }
+        xs[at] = from_float<T>(live ? v : 0.f);  // where x was
+      }
+    }
     __syncthreads();
-    float y[kTile];
-#pragma unroll
-    for (int s = 0; s < NS; ++s) {
-      float bt[kTile], ct[kTile];
-      tile_of(bs, s * 16 + p.j, bt);
-      if (!STATES_ONLY) tile_of(cs, s * 16 + p.j, ct);
-      unroll<kTile>([&](auto i) {
-        constexpr int I = decltype(i)::value;
-        const float a = exp2_of(lane_of_row<I>(k.delta) * A[s]);
-        h[s] = fmaf(a, h[s], lane_of_row<I>(in) * bt[I]);
-        if (!STATES_ONLY) y[I] = s ? fmaf(ct[I], h[s], y[I]) : ct[I] * h[s];
-      });
-    }
-    if (!STATES_ONLY) {
-      wave_fence();
-#pragma unroll
-      for (int i = 0; i < kTile; ++i) sums[wave][i * kSumPitch + lane] = y[i];
-      wave_fence();
-      float v = row_sum(sums[wave], lane) + skip * k.x;
-      if (c.gate.p) v *= gate * sigmoid(gate);
-      if (mine && t < c.T) *at<T>(c.y, p.b, t, d) = from_float<T>(live ? v : 0.f);
-    }
   }
-  if (!mine) return;
+  if (!STATES_ONLY) {
+    if (p.first < p.alive) {
+      out.take(raw);
+      out.store(p.last - p.first - (p.alive - p.first - 1) / TOKENS * TOKENS);
+    }
+    store_zeros<T, CH, F::THREADS>(c.out[0], p, d0, width, TOKENS);
+  }
+  if (!mine || tile) return;
   if (STATES_ONLY) {
 #pragma unroll
     for (int s = 0; s < NS; ++s)
@@ -139,13 +223,13 @@ __global__ __launch_bounds__(256) void scan_step_kernel(ScanCall c) {
   float y = 0.f, x = 0.f;
   if (slot >= 0) {
     const int g = (int)(d / c.E);
-    const Token k = token_of<T>(c, true, at<T>(c.x, b, 0, d), at<T>(c.dt, b, 0, d), c.dt_bias ? c.dt_bias[d] : 0.f);
+    const Token k = token_of(c, to_float(*at<T>(c.in[0], b, 0, d)), to_float(*at<T>(c.in[1], b, 0, d)), true, c.dt_bias ? c.dt_bias[d] : 0.f);
     x = k.x;
     if (n < c.N) {
       float* state = c.s_out + (slot * c.D + d) * c.N + n;
       fv h = *(const fv*)state;
       const fv A = *(const fv*)(c.A + d * c.N + n);
-      const T *pb = at<T>(c.b, b, 0, g, n), *pc = at<T>(c.c, b, 0, g, n);
+      const T *pb = at<T>(c.bc[0], b, 0, g, n), *pc = at<T>(c.bc[1], b, 0, g, n);
 #pragma unroll
       for (int s = 0; s < V; ++s) {
         h[s] = fmaf(exp2_of(k.delta * (A[s] * kLog2e)), h[s], k.delta * k.x * to_float(pb[s]));
@@ -159,50 +243,65 @@ __global__ __launch_bounds__(256) void scan_step_kernel(ScanCall c) {
   if (!live || i % L) return;
   if (slot >= 0) {
     if (c.skip) y = fmaf(c.skip[d], x, y);
-    if (c.gate.p) {
-      const float gate = to_float(*at<T>(c.gate, b, 0, d));
+    if (c.in[2].p) {
+      const float gate = to_float(*at<T>(c.in[2], b, 0, d));
       y *= gate * sigmoid(gate);
     }
   }
-  *at<T>(c.y, b, 0, d) = from_float<T>(y);
+  *at<T>(c.out[0], b, 0, d) = from_float<T>(y);
 }
 
 int states_of(const ScanCall& c) { return c.N <= 16 ? 1 : c.N <= 32 ? 2 : 4; }
-int blocks_of(const ScanCall& c) { return (int)cdiv(c.E, kChannels); }
 
-// Segments: as many as give the chip two wavefronts a SIMD, of 4 tiles at least
-int segments(const ScanCall& c, int64_t* tiles_of_one) {
-  const int64_t tiles = cdiv(c.T, kTile), groups = c.B * c.G * blocks_of(c);
-  int64_t n = groups ? 512 / groups : 1;
-  n = n < 1 ? 1 : n;
-  const int64_t most = cdiv(tiles, 4);
-  if (n > most) n = most > 0 ? most : 1;
-  *tiles_of_one = tiles > 0 ? cdiv(tiles, n) : 1;
-  return tiles > 0 ? (int)cdiv(tiles, *tiles_of_one) : 1;
+// Tiles at once (1: in turn) and segments
+struct Plan {
+  int W, n;
+  int64_t tokens;  // of a segment
+};
+Plan plan(const ScanCall& c) {
+  const int ns = states_of(c);
+  const int64_t rows = c.B * c.D;  // of 16 lanes
+  Plan z{};
+  z.W = ns == 4 || rows >= 16384 ? 1 : rows >= 4096 ? 4 : 8;
+  const int block = z.W == 8 ? 128 : ns == 4 ? 32 : 64, ch = z.W == 1 ? 16 : 8;
+  const int64_t in_all = cdiv(c.T, block), groups = c.B * c.G * cdiv(c.E, ch);
+  int64_t n = groups ? (z.W == 8 ? 128 : z.W == 4 ? 256 : 512) / groups : 1;
+  if (n > in_all) n = in_all;
+  if (n < 1) n = 1;
+  const int64_t each = in_all ? cdiv(in_all, n) : 1;
+  z.tokens = each * block;
+  z.n = in_all ? (int)cdiv(in_all, each) : 1;
+  return z;
 }
 
-template <typename T, int NS>
+template <typename T, int NS, typename F, bool STATES_ONLY>
 mdh_status pass(const ScanCall& c, const Segments& segs, hipStream_t st) {
-  const int blocks = blocks_of(c);
+  const int blocks = (int)cdiv(c.E, F::CH);
   const int64_t grid = c.B * segs.n * c.G * blocks;
-  if (grid >= 1 << 24) return MDH_ERR_SIZE;
+  if (grid * F::THREADS >= (int64_t)1 << 32) return MDH_ERR_SIZE;
   clear_stale_error();
-  if (segs.n > 1) {
-    scan_kernel<T, NS, true><<<(unsigned)grid, kThreads, 0, st>>>(c, segs, blocks);
-    mdh_status r = launch_status();
-    if (r != MDH_OK) return r;
-    r = launch_scan_segments(c, segs.h, segs.sum, segs.n, c.s_in, false, st);
-    if (r != MDH_OK) return r;
-  }
-  scan_kernel<T, NS, false><<<(unsigned)grid, kThreads, 0, st>>>(c, segs, blocks);
+  scan_kernel<T, NS, F, STATES_ONLY><<<(unsigned)grid, F::THREADS, 0, st>>>(c, segs, blocks);
   return launch_status();
 }
+template <typename T, int NS>
+mdh_status passes(const ScanCall& c, const Plan& z, const Segments& segs, hipStream_t st) {
+  if (segs.n > 1) {
+    mdh_status r = pass<T, NS, InTurn<NS>, true>(c, segs, st);
+    if (r == MDH_OK) r = launch_scan_segments(c, segs.h, segs.sum, segs.n, c.s_in, false, st);
+    if (r != MDH_OK) return r;
+  }
+  if constexpr (NS < 4) {
+    if (z.W == 4) return pass<T, NS, AtOnce<NS>, false>(c, segs, st);
+    if (z.W == 8) return pass<T, NS, ManyAtOnce<NS>, false>(c, segs, st);
+  }
+  return pass<T, NS, InTurn<NS>, false>(c, segs, st);
+}
 template <typename T>
-mdh_status pass_of(const ScanCall& c, const Segments& segs, hipStream_t st) {
+mdh_status pass_of(const ScanCall& c, const Plan& z, const Segments& segs, hipStream_t st) {
   switch (states_of(c)) {
-    case 1: return pass<T, 1>(c, segs, st);
-    case 2: return pass<T, 2>(c, segs, st);
-    default: return pass<T, 4>(c, segs, st);
+    case 1: return passes<T, 1>(c, z, segs, st);
+    case 2: return passes<T, 2>(c, z, segs, st);
+    default: return passes<T, 4>(c, z, segs, st);
   }
 }
 
@@ -239,16 +338,16 @@ mdh_status launch_scan_segments(const ScanCall& c, float* h, float* sum, int n, 
 }
 
 size_t scan_workspace(const ScanCall& c) {
-  int64_t tiles;
-  const int n = segments(c, &tiles);
+  const int n = plan(c).n;
   return n > 1 ? (size_t)(c.B * n) * (size_t)c.D * (size_t)(c.N + 1) * sizeof(float) : 0;
 }
 mdh_status launch_scan_forward(const ScanCall& c, hipStream_t st) {
+  const Plan z = plan(c);
   Segments segs{};
-  segs.n = segments(c, &segs.tiles);
+  segs.n = z.n, segs.tokens = z.tokens;
   segs.h = (float*)c.ws;
   segs.sum = segs.h + c.B * segs.n * (int64_t)c.D * c.N;
-  return c.dtype == MDH_BF16 ? pass_of<bf16>(c, segs, st) : pass_of<float>(c, segs, st);
+  return c.dtype == MDH_BF16 ? pass_of<bf16>(c, z, segs, st) : pass_of<float>(c, z, segs, st);
 }
 mdh_status launch_scan_step(const ScanCall& c, hipStream_t st) { return c.dtype == MDH_BF16 ? step_of<bf16>(c, st) : step_of<float>(c, st); }
 

@@ -5,37 +5,49 @@
 // a tile's a_t and h_t are computed again and stay in registers while it is walked back.
 //
 // 1 exponential and 15 multiplications a step: bound by the vector ALU.  De-composition as in the forward pass (a row of 16 lanes is a
-// channel, a lane a state); a workgroup has 64 channels, a row two of them one after the other.  Sums over the states (p, r,
-// sum q A) go through LDS, token j's to lane j.  Sums over the channels (d_b, d_c): a lane adds up its channels in registers, the
-// workgroup its rows in LDS at the end of a tile, a second launch the workgroups, in order.  Sums over tokens (d_A, d_skip, d_dt_bias)
+// channel, a lane a state); a workgroup has 32 channels.  Sums over the states (p, r,
+// sum q A) go through LDS, token j's to lane j.  Sums over the channels (d_b, d_c) go the same way, over the wavefront's rows, then the
+// workgroup's wavefronts; a second launch adds up the workgroups, in order.  Sums over tokens (d_A, d_skip, d_dt_bias)
 // stay in registers to the end of the segment.
 #include "mdh_selective.h"
 
 namespace mdh {
 namespace {
 
-constexpr int kThreads = 512, kWaves = kThreads / 64, kRows = kThreads / 16, kTimes = 2, kChannels = kRows * kTimes;
+constexpr int kThreads = 256, kRows = kThreads / 16;  // of the kernel over segments
 
 struct Parts {
   float *e, *sum;     // gradients of the states that the segments end with; sums of deltas of the segments
   float *shared;      // d_b, then d_c: (block, b, t, g, n)
   float *params;      // (b, seg): d_A, d_skip, d_dt_bias
   int n;
-  int64_t tiles;
+  int64_t tokens;  // of a segment
 };
 
 __device__ __forceinline__ float gate_of(float g) { return g * sigmoid(g); }
+// the last block of tokens that has a valid one
+__device__ __forceinline__ int64_t last_block(const ScanPlace& p, int block) {
+  return p.alive > p.first ? p.first + (p.alive - p.first - 1) / block * block : p.first - block;
+}
+
+constexpr int kTokens = 32;  // of a block
 
 // what a segment hands to the one before it, from zeros behind it
-constexpr int kSegThreads = 256;
 template <typename T, int NS>
-__global__ __launch_bounds__(kSegThreads) void grad_segments_kernel(ScanCall c, Parts w, int blocks) {
+__global__ __launch_bounds__(kThreads) void grad_segments_kernel(ScanCall c, Parts w, int blocks) {
   constexpr int S = NS * 16;
-  __shared__ float cs[S * kPitch];
-  const ScanPlace p = scan_place(c, blocks, w.n, w.tiles);
-  const int e0 = p.block * (kSegThreads / 16) + p.row;
-  const bool mine = e0 < c.E;
-  const int64_t d = (int64_t)p.g * c.E + e0;
+  typedef Stage<T, 3, 1, kRows, S, kTokens, kThreads> In;
+  __shared__ T raw[3 * kTokens * kRows] __attribute__((aligned(16)));
+  __shared__ float cs[In::kFloats] __attribute__((aligned(16)));
+  T *const dts = raw, *const gates = raw + kTokens * kRows, *const dys = raw + 2 * kTokens * kRows;
+  const ScanPlace p = scan_place(c, blocks, w.n, w.tokens);
+  const int e0 = p.block * kRows, width = min(kRows, c.E - e0);
+  const bool mine = p.row < width;
+  const int64_t d0 = (int64_t)p.g * c.E + e0, d = d0 + p.row;
+  In in;
+  int64_t t0 = last_block(p, kTokens);
+  in.begin(c.in + 1, c.bc + 1, p, t0, -1, d0, width, c.N);
+  if (t0 >= p.first) in.load(p.alive - t0);
   float A[NS], e[NS], total = 0.f;
 #pragma unroll
   for (int s = 0; s < NS; ++s) {
@@ -43,26 +55,29 @@ __global__ __launch_bounds__(kSegThreads) void grad_segments_kernel(ScanCall c, 
     e[s] = 0.f;
   }
   const float dt_bias = mine && c.dt_bias ? c.dt_bias[d] : 0.f;
-  for (int64_t tile = p.last - 1; tile >= p.first; --tile) {
-    const int64_t t0 = tile * kTile, t = t0 + p.j;
-    if (t0 >= p.len) continue;
-    const bool live = mine && t < p.len;
-    const Token k = token_of<T>(c, live, at<T>(c.x, p.b, t, d), at<T>(c.dt, p.b, t, d), dt_bias);
-    float dp = live ? to_float(*at<T>(c.y, p.b, t, d)) : 0.f;
-    if (c.gate.p && live) dp *= gate_of(to_float(*at<T>(c.gate, p.b, t, d)));
-    total += k.delta;
+  for (; t0 >= p.first; t0 -= kTokens) {
+    in.stage(raw, cs);
     __syncthreads();
-    stage_shared<T, S, kSegThreads>(c, c.c, p, t0, cs);
-    __syncthreads();
+    if (t0 > p.first) in.load(kTokens);
+    const int tokens = (int)min((int64_t)kTokens, p.alive - t0);
+    for (int i0 = (tokens - 1) / kTile * kTile; i0 >= 0; i0 -= kTile) {
+      const int at = place_of<T, kRows>(i0 + p.j, p.row);
+      const Token k = token_of(c, 0.f, to_float(dts[at]), i0 + p.j < tokens, dt_bias);
+      float dp = to_float(dys[at]);
+      if (c.in[2].p) dp *= gate_of(to_float(gates[at]));
+      total += k.delta;
 #pragma unroll
-    for (int s = 0; s < NS; ++s) {
-      float ct[kTile];
-      tile_of(cs, s * 16 + p.j, ct);
-      unroll<kTile>([&](auto i) {
-        constexpr int I = kTile - 1 - decltype(i)::value;
-        e[s] = exp2_of(lane_of_row<I>(k.delta) * A[s]) * fmaf(lane_of_row<I>(dp), ct[I], e[s]);
-      });
+      for (int s = 0; s < NS; ++s)
+        unroll<kTile / 4>([&](auto quarter) {
+          constexpr int Q = kTile - 4 - decltype(quarter)::value * 4;
+          const Float4 ct = four_of(cs + (s * 16 + p.j) * In::kPitch + i0 + Q);
+          unroll<4>([&](auto i) {
+            constexpr int I = 3 - decltype(i)::value;
+            e[s] = exp2_of(lane_of_row<Q + I>(k.delta) * A[s]) * fmaf(lane_of_row<Q + I>(dp), ct[I], e[s]);
+          });
+        });
     }
+    __syncthreads();
   }
   if (!mine) return;
   const int64_t seg = p.b * w.n + p.seg;
@@ -74,246 +89,269 @@ __global__ __launch_bounds__(kSegThreads) void grad_segments_kernel(ScanCall c, 
   if (p.j == 0) w.sum[seg * c.D + d] = total;
 }
 
-template <typename T, int NS>
-__global__ __launch_bounds__(kThreads) void scan_backward_kernel(ScanCall c, Parts w, int blocks) {
-  constexpr int S = NS * 16;
-  __shared__ float bs[S * kPitch], cs[S * kPitch], sums[kWaves][kSumFloats];
-  const ScanPlace p = scan_place(c, blocks, w.n, w.tiles);
+// A lane owns one channel's state of every 16; WAVES wavefronts are CH = 4 WAVES channels.
+template <typename T, int NS, int WAVES>
+__global__ __launch_bounds__(64 * WAVES, 2) void scan_backward_kernel(ScanCall c, Parts w, int blocks) {
+  constexpr int S = NS * 16, CH = 4 * WAVES, THREADS = 64 * WAVES, TILES = kTokens / kTile;
+  typedef Stage<T, 4, 2, CH, S, kTokens, THREADS> In;
+  typedef Outputs<T, 3, CH, kTokens, THREADS> Out;
+  __shared__ T raw[4 * kTokens * CH] __attribute__((aligned(16)));
+  __shared__ float bc[2 * In::kFloats] __attribute__((aligned(16))), sums[WAVES][kSumFloats] __attribute__((aligned(16)));
+  T *const xs = raw, *const dts = raw + kTokens * CH, *const gates = raw + 2 * kTokens * CH, *const dys = raw + 3 * kTokens * CH;
+  const ScanPlace p = scan_place(c, blocks, w.n, w.tokens);
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
   const int64_t seg = p.b * w.n + p.seg;
-  int64_t d[kTimes];
-  bool mine[kTimes];
-  float A[kTimes][NS], e[kTimes][NS], dA[kTimes][NS], skip[kTimes], dt_bias[kTimes], d_skip[kTimes], d_bias[kTimes];
+  const int e0 = p.block * CH, width = min(CH, c.E - e0);
+  const bool mine = p.row < width;
+  const int64_t d0 = (int64_t)p.g * c.E + e0, d = d0 + p.row;
+  In in;
+  int64_t t0 = last_block(p, kTokens);
+  in.begin(c.in, c.bc, p, t0, -1, d0, width, c.N);
+  float A[NS], e[NS], dA[NS], next_h[TILES][NS], d_skip = 0.f, d_bias = 0.f;
+  auto load = [&](int64_t from) {
+    in.load(p.alive - from);
 #pragma unroll
-  for (int m = 0; m < kTimes; ++m) {
-    const int ch = p.block * kChannels + m * kRows + p.row;
-    mine[m] = ch < c.E;
-    d[m] = (int64_t)p.g * c.E + ch;
+    for (int i = 0; i < TILES; ++i)
 #pragma unroll
-    for (int s = 0; s < NS; ++s) {
-      const int n = s * 16 + p.j;
-      const bool has = mine[m] && n < c.N;
-      A[m][s] = has ? c.A[d[m] * c.N + n] * kLog2e : 0.f;
-      e[m][s] = dA[m][s] = 0.f;
-      if (has && w.n > 1)
-        e[m][s] = w.e[(seg * c.D + d[m]) * c.N + n];
-      else if (has && c.s_in)
-        e[m][s] = c.s_in[(p.b * c.D + d[m]) * c.N + n];
-    }
-    skip[m] = mine[m] && c.skip ? c.skip[d[m]] : 0.f;
-    dt_bias[m] = mine[m] && c.dt_bias ? c.dt_bias[d[m]] : 0.f;
-    d_skip[m] = d_bias[m] = 0.f;
-  }
-  for (int64_t tile = p.last - 1; tile >= p.first; --tile) {
-    const int64_t t0 = tile * kTile, t = t0 + p.j;
-    if (t0 >= p.len) {
-#pragma unroll
-      for (int m = 0; m < kTimes; ++m)
-        if (mine[m] && t < c.T) {
-          *at<T>(c.dx, p.b, t, d[m]) = from_float<T>(0.f);
-          *at<T>(c.ddt, p.b, t, d[m]) = from_float<T>(0.f);
-          if (c.dgate.p) *at<T>(c.dgate, p.b, t, d[m]) = from_float<T>(0.f);
-        }
-      continue;
-    }
-    Token k[kTimes];
-    float gate[kTimes], dy[kTimes], dp[kTimes], sp[kTimes], sr[kTimes], sq[kTimes];
-#pragma unroll
-    for (int m = 0; m < kTimes; ++m) {
-      const bool live = mine[m] && t < p.len;
-      k[m] = token_of<T>(c, live, at<T>(c.x, p.b, t, d[m]), at<T>(c.dt, p.b, t, d[m]), dt_bias[m]);
-      dp[m] = dy[m] = live ? to_float(*at<T>(c.y, p.b, t, d[m])) : 0.f;
-      gate[m] = 0.f;
-      if (c.gate.p && live) {
-        gate[m] = to_float(*at<T>(c.gate, p.b, t, d[m]));
-        dp[m] *= gate_of(gate[m]);
+      for (int s = 0; s < NS; ++s) {
+        next_h[i][s] = 0.f;
+        if (mine && s * 16 + p.j < c.N && from + i * kTile < p.alive)
+          next_h[i][s] = c.checkpoints[((p.b * c.tiles + from / kTile + i) * c.D + d) * c.N + s * 16 + p.j];
       }
-      sp[m] = sr[m] = sq[m] = 0.f;
-    }
+  };
+  if (t0 >= p.first) load(t0);
+#pragma unroll
+  for (int s = 0; s < NS; ++s) {
+    const int n = s * 16 + p.j;
+    const bool has = mine && n < c.N;
+    A[s] = has ? c.A[d * c.N + n] * kLog2e : 0.f;
+    e[s] = dA[s] = 0.f;
+    if (has && w.n > 1)
+      e[s] = w.e[(seg * c.D + d) * c.N + n];
+    else if (has && c.s_in)
+      e[s] = c.s_in[(p.b * c.D + d) * c.N + n];
+  }
+  const float skip = mine && c.skip ? c.skip[d] : 0.f, dt_bias = mine && c.dt_bias ? c.dt_bias[d] : 0.f;
+  for (int i = 0; i < 3; ++i)
+    if (c.out[i].p) store_zeros<T, CH, THREADS>(c.out[i], p, d0, width, kTokens);
+  Out out;
+  out.begin(c.out, p, t0, -1, d0, width);
+  bool behind = false;  // a block's gradients lie in LDS
+  for (; t0 >= p.first; t0 -= kTokens) {
+    if (behind) out.take(raw);
+    in.stage(raw, bc);
+    float h0[TILES][NS];
+#pragma unroll
+    for (int i = 0; i < TILES; ++i)
+#pragma unroll
+      for (int s = 0; s < NS; ++s) h0[i][s] = next_h[i][s];
     __syncthreads();
-    stage_shared<T, S, kThreads>(c, c.b, p, t0, bs);
-    stage_shared<T, S, kThreads>(c, c.c, p, t0, cs);
-    __syncthreads();
+    // (stores go out behind the wait for the block's loads: what is waited for next has been under way for long)
+    if (behind) out.store(p.last - t0 - kTokens);
+    behind = true;
+    if (t0 > p.first) load(t0 - kTokens);
+    const int tokens = (int)min((int64_t)kTokens, p.alive - t0);
 #pragma unroll
-    for (int s = 0; s < NS; ++s) {
-      float bt[kTile], ct[kTile], db[kTile], dc[kTile];
-      tile_of(bs, s * 16 + p.j, bt);
-      tile_of(cs, s * 16 + p.j, ct);
+    for (int tile = TILES - 1; tile >= 0; --tile) {
+      const int i0 = tile * kTile;
+      if (i0 >= tokens) continue;
+      const bool live = i0 + p.j < tokens;
+      const int at = place_of<T, CH>(i0 + p.j, p.row);
+      const Token k = token_of(c, to_float(xs[at]), to_float(dts[at]), live, dt_bias);
+      const float dy = to_float(dys[at]), dp = c.in[2].p ? dy * gate_of(to_float(gates[at])) : dy, u = k.delta * k.x;
+      float sp = 0.f, sr = 0.f, sq = 0.f;
+      float* own = sums[wave];
 #pragma unroll
-      for (int i = 0; i < kTile; ++i) db[i] = dc[i] = 0.f;
-#pragma unroll
-      for (int m = 0; m < kTimes; ++m) {
-        const float in = k[m].delta * k[m].x;
-        float h[kTile + 1], a[kTile];
-        h[0] = mine[m] && s * 16 + p.j < c.N ? c.checkpoints[((p.b * c.tiles + tile) * c.D + d[m]) * c.N + s * 16 + p.j] : 0.f;
+      for (int s = 0; s < NS; ++s) {
+        const float* bs = bc + (s * 16 + p.j) * In::kPitch + i0;
+        float h[kTile + 1], a[kTile], g[kTile];
+        h[0] = h0[tile][s];
+        unroll<kTile / 4>([&](auto quarter) {
+          constexpr int Q = decltype(quarter)::value * 4;
+          const Float4 bt = four_of(bs + Q), ct = four_of(bs + In::kFloats + Q);
+          unroll<4>([&](auto i) {
+            constexpr int I = Q + decltype(i)::value;
+            a[I] = exp2_of(lane_of_row<I>(k.delta) * A[s]);
+            h[I + 1] = fmaf(a[I], h[I], lane_of_row<I>(u) * bt[I - Q]);
+            own[I * kSumPitch + lane] = ct[I - Q] * h[I + 1];
+          });
+        });
+        wave_fence();
+        sp += row_sum(own, lane);
+        wave_fence();
+        const float dp2 = again(dp), delta2 = again(k.delta), u2 = again(u);
+        unroll<kTile>([&](auto i) {
+          constexpr int I = decltype(i)::value;
+          own[I * kSumPitch + lane] = lane_of_row<I>(dp) * h[I + 1];
+        });
+        wave_fence();
+        const Float4 dc = over_rows(own, lane);
+        wave_fence();
+        unroll<kTile / 4>([&](auto quarter) {
+          constexpr int Q = kTile - 4 - decltype(quarter)::value * 4;
+          const Float4 bt = four_of(bs + Q), ct = four_of(bs + In::kFloats + Q);
+          unroll<4>([&](auto i) {
+            constexpr int I = Q + 3 - decltype(i)::value;
+            g[I] = fmaf(lane_of_row<I>(dp2), ct[I - Q], e[s]);
+            own[I * kSumPitch + lane] = g[I] * bt[I - Q];
+            e[s] = a[I] * g[I];
+            a[I] = e[s] * h[I];  // (the factor is done with)
+            dA[s] = fmaf(lane_of_row<I>(delta2), a[I], dA[s]);
+          });
+        });
+        wave_fence();
+        sr += row_sum(own, lane);
         wave_fence();
         unroll<kTile>([&](auto i) {
           constexpr int I = decltype(i)::value;
-          a[I] = exp2_of(lane_of_row<I>(k[m].delta) * A[m][s]);
-          h[I + 1] = fmaf(a[I], h[I], lane_of_row<I>(in) * bt[I]);
-          sums[wave][I * kSumPitch + lane] = ct[I] * h[I + 1];
+          own[I * kSumPitch + lane] = lane_of_row<I>(u2) * g[I];
         });
         wave_fence();
-        sp[m] += row_sum(sums[wave], lane);
-        wave_fence();
-        float q[kTile];
-        unroll<kTile>([&](auto i) {
-          constexpr int I = kTile - 1 - decltype(i)::value;
-          const float g = fmaf(lane_of_row<I>(dp[m]), ct[I], e[m][s]);
-          dc[I] = fmaf(lane_of_row<I>(dp[m]), h[I + 1], dc[I]);
-          db[I] = fmaf(lane_of_row<I>(in), g, db[I]);
-          sums[wave][I * kSumPitch + lane] = g * bt[I];
-          e[m][s] = a[I] * g;
-          const float gh = e[m][s] * h[I];
-          dA[m][s] = fmaf(lane_of_row<I>(k[m].delta), gh, dA[m][s]);
-          q[I] = gh * A[m][s];
-        });
-        wave_fence();
-        sr[m] += row_sum(sums[wave], lane);
+        const Float4 db = over_rows(own, lane);
         wave_fence();
 #pragma unroll
-        for (int i = 0; i < kTile; ++i) sums[wave][i * kSumPitch + lane] = q[i];
+        for (int i = 0; i < kTile; ++i) own[i * kSumPitch + lane] = a[i] * A[s];
         wave_fence();
-        sq[m] += row_sum(sums[wave], lane);
-      }
-      // over the rows of the workgroup
-#pragma unroll
-      for (int which = 0; which < 2; ++which) {
+        sq += row_sum(own, lane);
         wave_fence();
+        // over the wavefronts
 #pragma unroll
-        for (int i = 0; i < kTile; ++i) sums[wave][i * kSumPitch + lane] = which ? dc[i] : db[i];
+        for (int i = 0; i < 4; ++i) own[i * 64 + lane] = db[i], own[256 + i * 64 + lane] = dc[i];
         __syncthreads();
-        const int i = threadIdx.x / 16, n = s * 16 + p.j;
-        if (threadIdx.x < 256) {
-          float v = 0.f;
 #pragma unroll
-          for (int x = 0; x < kWaves; ++x)
+        for (int i = threadIdx.x; i < 512; i += THREADS) {
+          const int which = i / 256, t = i / 16 % 4 * 4 + i / 64 % 4, n = s * 16 + i % 16;
+          float sum = sums[0][i];
 #pragma unroll
-            for (int r = 0; r < 4; ++r) v += sums[x][i * kSumPitch + r * 16 + p.j];
-          if (n < c.N && t0 + i < p.len)
-            w.shared[(((which * (int64_t)blocks + p.block) * c.B + p.b) * c.T + t0 + i) * c.G * c.N + (int64_t)p.g * c.N + n] = v;
+          for (int v = 1; v < WAVES; ++v) sum += sums[v][i];
+          if (n < c.N && i0 + t < tokens)
+            w.shared[(((which * (int64_t)blocks + p.block) * c.B + p.b) * c.T + t0 + i0 + t) * c.G * c.N + (int64_t)p.g * c.N + n] = sum;
         }
         __syncthreads();
       }
-    }
-#pragma unroll
-    for (int m = 0; m < kTimes; ++m) {
-      if (!mine[m] || t >= c.T) continue;
-      const bool live = t < p.len;
-      const float d_delta = fmaf(k[m].x, sr[m], sq[m] * kLn2);
-      const float d_dt = c.softplus ? d_delta * sigmoid(k[m].raw) : d_delta;
-      d_skip[m] = fmaf(dp[m], k[m].x, d_skip[m]);
-      if (live) d_bias[m] += d_dt;
-      *at<T>(c.dx, p.b, t, d[m]) = from_float<T>(live ? fmaf(k[m].delta, sr[m], skip[m] * dp[m]) : 0.f);
-      *at<T>(c.ddt, p.b, t, d[m]) = from_float<T>(live ? d_dt : 0.f);
-      if (c.dgate.p) {
-        const float f = sigmoid(gate[m]);
-        *at<T>(c.dgate, p.b, t, d[m]) =
-            from_float<T>(live ? dy[m] * fmaf(skip[m], k[m].x, sp[m]) * f * (1.f + gate[m] * (1.f - f)) : 0.f);
+      const float d_delta = fmaf(k.x, sr, sq * kLn2), d_dt = c.softplus ? d_delta * sigmoid(k.raw) : d_delta;
+      d_skip = fmaf(dp, k.x, d_skip);
+      if (live) d_bias += d_dt;
+      // gradients take the places of what they are the gradients of
+      xs[at] = from_float<T>(live ? fmaf(k.delta, sr, skip * dp) : 0.f);
+      dts[at] = from_float<T>(live ? d_dt : 0.f);
+      if (c.out[2].p) {
+        const float g = to_float(gates[at]), f = sigmoid(g);
+        gates[at] = from_float<T>(live ? dy * fmaf(skip, k.x, sp) * f * (1.f + g * (1.f - f)) : 0.f);
       }
     }
+    __syncthreads();
+  }
+  if (behind) {
+    out.take(raw);
+    out.store(p.last - p.first);
   }
   float* row = w.params + seg * c.D * (c.N + 2);
 #pragma unroll
-  for (int m = 0; m < kTimes; ++m) {
+  for (int k = 1; k < 16; k *= 2) d_skip += __shfl_xor(d_skip, k), d_bias += __shfl_xor(d_bias, k);
+  if (!mine) return;
 #pragma unroll
-    for (int k = 1; k < 16; k *= 2) d_skip[m] += __shfl_xor(d_skip[m], k), d_bias[m] += __shfl_xor(d_bias[m], k);
-    if (!mine[m]) continue;
-#pragma unroll
-    for (int s = 0; s < NS; ++s) {
-      const int n = s * 16 + p.j;
-      if (n >= c.N) continue;
-      row[d[m] * c.N + n] = dA[m][s];
-      if (p.seg == 0 && c.s_out) c.s_out[(p.b * c.D + d[m]) * c.N + n] = e[m][s];
-    }
-    if (p.j == 0) row[(int64_t)c.D * c.N + d[m]] = d_skip[m], row[(int64_t)c.D * (c.N + 1) + d[m]] = d_bias[m];
+  for (int s = 0; s < NS; ++s) {
+    const int n = s * 16 + p.j;
+    if (n >= c.N) continue;
+    row[d * c.N + n] = dA[s];
+    if (p.seg == 0 && c.s_out) c.s_out[(p.b * c.D + d) * c.N + n] = e[s];
   }
+  if (p.j == 0) row[(int64_t)c.D * c.N + d] = d_skip, row[(int64_t)c.D * (c.N + 1) + d] = d_bias;
 }
 
-// d_b and d_c: the blocks of channels of each group, in order
+// d_b and d_c: the blocks of channels of each group, in order.  blockIdx.y: which of the two
 template <typename T>
 __global__ __launch_bounds__(256) void shared_sums_kernel(ScanCall c, const float* part, int blocks) {
   const int64_t per = c.B * c.T * c.G * c.N, i = (int64_t)blockIdx.x * 256 + threadIdx.x;
   if (i >= per) return;
   const int n = (int)(i % c.N), g = (int)(i / c.N % c.G);
   const int64_t t = i / c.N / c.G % c.T, b = i / c.N / c.G / c.T;
-  const bool live = t < scan_length(c, b);
+  const float* p = part + blockIdx.y * (int64_t)blocks * per + i;
+  float v[4] = {0.f, 0.f, 0.f, 0.f};
+  if (t < scan_length(c, b)) {
+    int k = 0;
+    for (; k + 3 < blocks; k += 4)
 #pragma unroll
-  for (int which = 0; which < 2; ++which) {
-    const float* p = part + which * (int64_t)blocks * per + i;
-    float v = 0.f;
-    if (live)
-      for (int k = 0; k < blocks; ++k) v += p[k * per];
-    *at<T>(which ? c.dc : c.db, b, t, g, n) = from_float<T>(v);
+      for (int u = 0; u < 4; ++u) v[u] += p[(k + u) * per];
+    for (; k < blocks; ++k) v[0] += p[k * per];
   }
+  *at<T>(c.dbc[blockIdx.y], b, t, g, n) = from_float<T>((v[0] + v[1]) + (v[2] + v[3]));
 }
 
-int states_of(const ScanCall& c) { return c.N <= 16 ? 1 : c.N <= 32 ? 2 : 4; }
-int blocks_of(const ScanCall& c) { return (int)cdiv(c.E, kChannels); }
-
-// Segments: as many as give the chip two wavefronts a SIMD, of 4 tiles at least
-int segments(const ScanCall& c, int64_t* tiles_of_one) {
-  const int64_t tiles = cdiv(c.T, kTile), groups = c.B * c.G * blocks_of(c);
+// Wavefronts of a workgroup (the more, the fewer the rows of partial sums of d_b and d_c), and segments: of the tokens, as many as
+// give the chip two wavefronts a SIMD, whole blocks of tokens.
+struct Shape {
+  int NS, waves, blocks, n;  // blocks of 4 * waves channels of a group, segments
+  int64_t tokens;        // of a segment
+};
+Shape shape_of(const ScanCall& c) {
+  Shape z;
+  z.NS = c.N <= 16 ? 1 : c.N <= 32 ? 2 : 4;
+  z.waves = 8;
+  z.blocks = (int)cdiv(c.E, 4 * z.waves);
+  const int block = kTokens;
+  const int64_t in_all = cdiv(c.T, block), groups = c.B * c.G * z.blocks;
   int64_t n = groups ? 256 / groups : 1;
-  n = n < 1 ? 1 : n;
-  const int64_t most = cdiv(tiles, 4);
-  if (n > most) n = most > 0 ? most : 1;
-  *tiles_of_one = tiles > 0 ? cdiv(tiles, n) : 1;
-  return tiles > 0 ? (int)cdiv(tiles, *tiles_of_one) : 1;
+  if (n > in_all) n = in_all;
+  if (n < 1) n = 1;
+  const int64_t each = in_all ? cdiv(in_all, n) : 1;
+  z.tokens = each * block;
+  z.n = in_all ? (int)cdiv(in_all, each) : 1;
+  return z;
 }
 
 size_t up16(size_t n) { return (n + 15) & ~(size_t)15; }
 // bytes of: states and sums of the segments, d_b and d_c of the blocks, parameters' rows
-size_t seg_bytes(const ScanCall& c, int n) { return n > 1 ? up16((size_t)c.B * n * c.D * (c.N + 1) * sizeof(float)) : 0; }
-size_t shared_bytes(const ScanCall& c) { return up16((size_t)2 * blocks_of(c) * c.B * c.T * c.G * c.N * sizeof(float)); }
-size_t param_bytes(const ScanCall& c, int n) { return (size_t)c.B * n * c.D * (c.N + 2) * sizeof(float); }
+size_t seg_bytes(const ScanCall& c, const Shape& z) { return z.n > 1 ? up16((size_t)c.B * z.n * c.D * (c.N + 1) * sizeof(float)) : 0; }
+size_t shared_bytes(const ScanCall& c, const Shape& z) { return up16((size_t)2 * z.blocks * c.B * c.T * c.G * c.N * sizeof(float)); }
+size_t param_bytes(const ScanCall& c, const Shape& z) { return (size_t)c.B * z.n * c.D * (c.N + 2) * sizeof(float); }
 
-template <typename T, int NS>
-mdh_status pass(const ScanCall& c, const Parts& w, hipStream_t st) {
-  const int blocks = blocks_of(c), seg_blocks = (int)cdiv(c.E, kSegThreads / 16);
-  const int64_t grid = c.B * w.n * c.G * blocks, seg_grid = c.B * w.n * c.G * seg_blocks, outs = cdiv(c.B * c.T * c.G * c.N, 256);
-  if (grid >= 1 << 23 || (w.n > 1 && seg_grid >= 1 << 24) || outs >= 1 << 24) return MDH_ERR_SIZE;
+template <typename T, int NS, int WAVES>
+mdh_status pass(const ScanCall& c, const Shape& z, const Parts& w, hipStream_t st) {
+  const int seg_blocks = (int)cdiv(c.E, kRows);
+  const int64_t grid = c.B * z.n * c.G * z.blocks, seg_grid = c.B * z.n * c.G * seg_blocks, outs = cdiv(c.B * c.T * c.G * c.N, 256);
+  if (grid * z.waves >= 1 << 26 || (z.n > 1 && seg_grid >= 1 << 24) || outs >= 1 << 23) return MDH_ERR_SIZE;
   clear_stale_error();
-  if (w.n > 1) {
-    grad_segments_kernel<T, NS><<<(unsigned)seg_grid, kSegThreads, 0, st>>>(c, w, seg_blocks);
+  if (z.n > 1) {
+    grad_segments_kernel<T, NS><<<(unsigned)seg_grid, kThreads, 0, st>>>(c, w, seg_blocks);
     mdh_status r = launch_status();
     if (r != MDH_OK) return r;
     r = launch_scan_segments(c, w.e, w.sum, w.n, c.s_in, true, st);
     if (r != MDH_OK) return r;
   }
-  scan_backward_kernel<T, NS><<<(unsigned)grid, kThreads, 0, st>>>(c, w, blocks);
-  mdh_status r = launch_status();
+  scan_backward_kernel<T, NS, WAVES><<<(unsigned)grid, 64 * WAVES, 0, st>>>(c, w, z.blocks);
+  const mdh_status r = launch_status();
   if (r != MDH_OK || outs == 0) return r;
-  shared_sums_kernel<T><<<(unsigned)outs, 256, 0, st>>>(c, w.shared, blocks);
+  shared_sums_kernel<T><<<dim3((unsigned)outs, 2), 256, 0, st>>>(c, w.shared, z.blocks);
   return launch_status();
 }
 template <typename T>
-mdh_status pass_of(const ScanCall& c, const Parts& w, hipStream_t st) {
-  switch (states_of(c)) {
-    case 1: return pass<T, 1>(c, w, st);
-    case 2: return pass<T, 2>(c, w, st);
-    default: return pass<T, 4>(c, w, st);
+mdh_status pass_of(const ScanCall& c, const Shape& z, const Parts& w, hipStream_t st) {
+  switch (z.NS) {
+    case 1: return pass<T, 1, 8>(c, z, w, st);
+    case 2: return pass<T, 2, 8>(c, z, w, st);
+    default: return pass<T, 4, 8>(c, z, w, st);
   }
 }
 
 }  // namespace
 
 size_t scan_backward_workspace(const ScanCall& c) {
-  if (c.B == 0) return 0;
-  int64_t tiles;
-  const int n = segments(c, &tiles);
-  return seg_bytes(c, n) + shared_bytes(c) + param_bytes(c, n);
+  const Shape z = shape_of(c);
+  return c.B ? seg_bytes(c, z) + shared_bytes(c, z) + param_bytes(c, z) : 0;
 }
 mdh_status launch_scan_backward(const ScanCall& c, hipStream_t st) {
+  const Shape z = shape_of(c);
   Parts w{};
-  w.n = segments(c, &w.tiles);
+  w.n = z.n, w.tokens = z.tokens;
   int64_t rows = 0;
   if (c.B) {
     w.e = (float*)c.ws, w.sum = w.e + c.B * w.n * (int64_t)c.D * c.N;
-    w.shared = (float*)((char*)c.ws + seg_bytes(c, w.n));
-    w.params = (float*)((char*)w.shared + shared_bytes(c));
+    w.shared = (float*)((char*)c.ws + seg_bytes(c, z));
+    w.params = (float*)((char*)w.shared + shared_bytes(c, z));
     rows = c.B * w.n;
-    const mdh_status r = c.dtype == MDH_BF16 ? pass_of<bf16>(c, w, st) : pass_of<float>(c, w, st);
+    const mdh_status r = c.dtype == MDH_BF16 ? pass_of<bf16>(c, z, w, st) : pass_of<float>(c, z, w, st);
     if (r != MDH_OK) return r;
   }
   const int64_t states = (int64_t)c.D * c.N;
