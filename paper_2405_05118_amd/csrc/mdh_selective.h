@@ -27,6 +27,8 @@ template <int J>
 __device__ __forceinline__ float lane_of_row(float v) {
   return __int_as_float(__builtin_amdgcn_mov_dpp(__float_as_int(v), 0x150 + J, 0xf, 0xf, true));
 }
+// computed here, not behind the next barrier with all that it is computed from in registers until there
+__device__ __forceinline__ void settle(float& v) { asm volatile("" : "+v"(v)); }
 // The same value to be broadcast at another place: where the compiler knows that two broadcasts are one, it keeps their result in
 // a register of its own, 16 for a tile, and both lose the modifier.
 __device__ __forceinline__ float again(float v) {

@@ -258,14 +258,23 @@ struct Plan {
   int W, n;
   int64_t tokens;  // of a segment
 };
+// The least of estimated times, in cycles for 16 states.  In turn: 55 a token and 60 for every wavefront of a SIMD (one of them: 2048
+// tokens of 4096 channels 116 us; four: 4 x 2048 of 4096 234).  At once: 98 a token with two workgroups of 8 wavefronts a compute unit,
+// 65 with one (84 us), 60 with one of 16 (32768 of 1536 channels: 826).  Segments: 92 a step whatever the shape, and two more launches
+// (32768 of 1536: 474; 2048 of 4096: 99).
 Plan plan(const ScanCall& c) {
   const int ns = states_of(c);
-  const int64_t rows = c.B * c.D;  // of 16 lanes
-  Plan z{};
-  z.W = ns == 4 || rows >= 16384 ? 1 : rows >= 4096 ? 4 : 8;
-  const int block = z.W == 8 ? 128 : ns == 4 ? 32 : 64, ch = z.W == 1 ? 16 : 8;
-  const int64_t in_all = cdiv(c.T, block), groups = c.B * c.G * cdiv(c.E, ch);
-  int64_t n = groups ? (z.W == 8 ? 128 : z.W == 4 ? 256 : 512) / groups : 1;
+  const int64_t T = c.T, eights = c.B * c.G * cdiv(c.E, 8), groups = c.B * c.G * cdiv(c.E, 16);
+  const int64_t turn = T * (55 + (groups * 60 + 255) / 256), four = T * (eights <= 256 ? 65 : 98 * cdiv(eights, 512)), eight = T * 60 * cdiv(eights, 256);
+  const int64_t cut = T * groups * 92 / 256 + 24000;
+  Plan z{1, 1, 0};
+  int64_t best = turn;
+  if (ns < 4 && four < best) z.W = 4, best = four;
+  if (ns < 4 && eight < best) z.W = 8, best = eight;
+  if (cut < best) z.W = 1;
+  const int block = z.W == 8 ? 128 : ns == 4 ? 32 : 64;
+  const int64_t in_all = cdiv(T, block);
+  int64_t n = cut < best ? cdiv(3072, groups) : 1;
   if (n > in_all) n = in_all;
   if (n < 1) n = 1;
   const int64_t each = in_all ? cdiv(in_all, n) : 1;

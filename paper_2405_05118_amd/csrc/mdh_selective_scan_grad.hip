@@ -91,7 +91,7 @@ __global__ __launch_bounds__(kThreads) void grad_segments_kernel(ScanCall c, Par
 
 // A lane owns one channel's state of every 16; WAVES wavefronts are CH = 4 WAVES channels.
 template <typename T, int NS, int WAVES>
-__global__ __launch_bounds__(64 * WAVES, 2) void scan_backward_kernel(ScanCall c, Parts w, int blocks) {
+__global__ __launch_bounds__(64 * WAVES, NS == 1 && sizeof(T) == 2 ? 4 : 2) void scan_backward_kernel(ScanCall c, Parts w, int blocks) {
   constexpr int S = NS * 16, CH = 4 * WAVES, THREADS = 64 * WAVES, TILES = kTokens / kTile;
   typedef Stage<T, 4, 2, CH, S, kTokens, THREADS> In;
   typedef Outputs<T, 3, CH, kTokens, THREADS> Out;
@@ -178,6 +178,7 @@ __global__ __launch_bounds__(64 * WAVES, 2) void scan_backward_kernel(ScanCall c
         });
         wave_fence();
         sp += row_sum(own, lane);
+        settle(sp);
         wave_fence();
         const float dp2 = again(dp), delta2 = again(k.delta), u2 = again(u);
         unroll<kTile>([&](auto i) {
@@ -201,6 +202,7 @@ __global__ __launch_bounds__(64 * WAVES, 2) void scan_backward_kernel(ScanCall c
         });
         wave_fence();
         sr += row_sum(own, lane);
+        settle(sr), settle(dA[s]), settle(e[s]);
         wave_fence();
         unroll<kTile>([&](auto i) {
           constexpr int I = decltype(i)::value;
@@ -213,6 +215,7 @@ __global__ __launch_bounds__(64 * WAVES, 2) void scan_backward_kernel(ScanCall c
         for (int i = 0; i < kTile; ++i) own[i * kSumPitch + lane] = a[i] * A[s];
         wave_fence();
         sq += row_sum(own, lane);
+        settle(sq);
         wave_fence();
         // over the wavefronts
 #pragma unroll
