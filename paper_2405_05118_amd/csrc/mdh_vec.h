@@ -1,23 +1,31 @@
-// Rows of V = 16 / sizeof(T) channels a lane, at any alignment that the type has: 16 bytes at a time (the hardware reads and
+// Rows of V channels a lane (16 bytes, or 8), at any alignment that the type has: all at a time (the hardware reads and
 // writes unaligned ones, in one or two pieces), the last channels of a row that has no V left one by one.
 #pragma once
 #include "mdh_types.h"
 
 namespace mdh {
 
-typedef uint32_t Word4 __attribute__((ext_vector_type(4)));
-typedef Word4 AnyWord4 __attribute__((aligned(2)));
+template <int N>
+struct WordsOf {
+  typedef uint32_t type __attribute__((ext_vector_type(N)));
+  typedef type any __attribute__((aligned(2)));
+};
+template <int N>
+using Words = typename WordsOf<N>::type;
+typedef Words<4> Word4;
 typedef float Float4 __attribute__((ext_vector_type(4)));
 typedef Float4 AnyFloat4 __attribute__((aligned(4)));
 
 template <typename T>
 constexpr int kLaneValues = 16 / (int)sizeof(T);
+// V values of a lane as they are in memory
+template <typename T, int V>
+using RowWords = Words<V * (int)sizeof(T) / 4>;
 
-template <typename T>
-__device__ __forceinline__ Word4 load_row(const T* p, int left) {
-  constexpr int V = kLaneValues<T>;
-  if (left >= V) return *(const AnyWord4*)p;
-  Word4 w = {0, 0, 0, 0};
+template <typename T, int V = kLaneValues<T>>
+__device__ __forceinline__ RowWords<T, V> load_row(const T* p, int left) {
+  if (left >= V) return *(const typename WordsOf<V * (int)sizeof(T) / 4>::any*)p;
+  RowWords<T, V> w = 0;
 #pragma unroll
   for (int i = 0; i < V - 1; ++i)
     if (i < left) {
@@ -28,11 +36,10 @@ __device__ __forceinline__ Word4 load_row(const T* p, int left) {
     }
   return w;
 }
-template <typename T>
-__device__ __forceinline__ void store_row(T* p, int left, const Word4& w) {
-  constexpr int V = kLaneValues<T>;
+template <typename T, int V = kLaneValues<T>>
+__device__ __forceinline__ void store_row(T* p, int left, const RowWords<T, V>& w) {
   if (left >= V) {
-    *(AnyWord4*)p = w;
+    *(typename WordsOf<V * (int)sizeof(T) / 4>::any*)p = w;
     return;
   }
 #pragma unroll
@@ -44,21 +51,21 @@ __device__ __forceinline__ void store_row(T* p, int left, const Word4& w) {
         ((uint16_t*)p)[i] = (uint16_t)(w[i / 2] >> 16 * (i & 1));
     }
 }
-template <typename T>
-__device__ __forceinline__ void unpack_row(const Word4& w, float (&x)[kLaneValues<T>]) {
+template <typename T, int V = kLaneValues<T>>
+__device__ __forceinline__ void unpack_row(const RowWords<T, V>& w, float (&x)[V]) {
 #pragma unroll
-  for (int i = 0; i < kLaneValues<T>; ++i) {
+  for (int i = 0; i < V; ++i) {
     if constexpr (sizeof(T) == 4)
       x[i] = __uint_as_float(w[i]);
     else
       x[i] = __uint_as_float(i & 1 ? w[i / 2] & 0xffff0000u : w[i / 2] << 16);
   }
 }
-template <typename T>
-__device__ __forceinline__ Word4 pack_row(const float (&x)[kLaneValues<T>]) {
-  Word4 w;
+template <typename T, int V = kLaneValues<T>>
+__device__ __forceinline__ RowWords<T, V> pack_row(const float (&x)[V]) {
+  RowWords<T, V> w;
 #pragma unroll
-  for (int i = 0; i < 4; ++i) {
+  for (int i = 0; i < V * (int)sizeof(T) / 4; ++i) {
     if constexpr (sizeof(T) == 4)
       w[i] = __float_as_uint(x[i]);
     else
