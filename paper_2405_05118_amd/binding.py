@@ -706,12 +706,13 @@ def mdh_selective_scan_checkpoints_size(sizes: Sequence[int]) -> int:
 def _scan_operands(lead, x, A, b, c, dt, *alike):
     """Sizes behind the leading ones; every tensor of ``alike`` has x's shape, b and c (*lead, G, N)."""
     D, N = A.shape
-    if x.shape != (*lead, D):
+    shape, shared = x.shape, b.shape
+    if shape != (*lead, D):
         raise _unfit(("x", x), ("A", A))
-    if len(b.shape) != len(lead) + 2 or b.shape[:-2] != lead or b.shape[-1] != N or c.shape != b.shape:
+    if len(shared) != len(lead) + 2 or shared[:-2] != lead or shared[-1] != N or c.shape != shared:
         raise _unfit(("A", A), ("b", b), ("c", c))
-    _same(x.shape, (dt, "dt"), *alike)
-    return D, N, b.shape[-2]
+    _same(shape, (dt, "dt"), *alike)
+    return D, N, shared[-2]
 
 
 def mdh_selective_scan(x, dt, A, b, c, y, skip=None, gate=None, dt_bias=None, softplus: bool = False, lengths=None, initial_state=None,
@@ -767,11 +768,18 @@ def mdh_selective_scan_step(x, dt, A, b, c, state, y, skip=None, gate=None, dt_b
     """One token with the state in place.  x, dt, gate, y: (B, D); b, c: (B, G, N); state: (B, D, N) float32, or with slots (B,) int32
     a pool (n, D, N)."""
     L = _lib or lib()
-    B = x.shape[0]
-    D, N, G = _scan_operands((B,), x, A, b, c, dt, (y, "y"), (gate, "gate"))
+    B, D = shape = x.shape
+    N, G = A.shape[1], b.shape[1]
+    shared = (B, G, N)  # (a call is as fast as the host is: nothing is looked at twice)
+    if (A.shape[0] != D or dt.shape != shape or y.shape != shape or b.shape != shared or c.shape != shared
+            or (gate is not None and gate.shape != shape)):
+        _scan_operands((B,), x, A, b, c, dt, (y, "y"), (gate, "gate"))
     ty = x.dtype
     d = _dtype_of(ty)
-    (sp,), n, slots_p = _pools(B, (D, N), _F32, slots, (state, "state"))
+    if slots is None:
+        sp, n, slots_p = _opt(state, _F32, "state", (B, D, N)), 0, None
+    else:
+        (sp,), n, slots_p = _pools(B, (D, N), _F32, slots, (state, "state"))
     st = L.mdh_selective_scan_step(_q4(B, D, N, G), d, _strided(x, ty, "x"), _strided(dt, ty, "dt"), _sp(gate, ty, "gate"),
                                    _strided(b, ty, "b"), _strided(c, ty, "c"), _strides((x, dt, x if gate is None else gate, y, b, c)),
                                    _opt(A, _F32, "A"), _opt(skip, _F32, "skip", (D,)), _opt(dt_bias, _F32, "dt_bias", (D,)), int(softplus),

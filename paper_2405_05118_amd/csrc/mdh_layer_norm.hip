@@ -183,47 +183,62 @@ __global__ __launch_bounds__(L > 256 ? L : 256) void layer_norm_backward_kernel(
     for (int i = 0; i < V; ++i) dw[k][i] = db[k][i] = 0.f;
   }
   const float over = 1.f / (float)c.C;
-  for (int64_t first = (int64_t)blockIdx.x * R; first < c.rows; first += (int64_t)gridDim.x * R) {
-    const int64_t row = first + threadIdx.x / L;
+  struct Row {
+    Word4 x[P], y[P], t[P];
+    float mean, rstd;
+  };
+  // the next row is under way while one is worked on
+  auto load = [&](Row& r, int64_t row) {
     const bool live = row < c.rows;
-    const float mean = live ? c.mean[row] : 0.f, rstd = live ? c.rstd[row] : 0.f;
-    Word4 rx[P], ry[P], rt[P];
+    r.mean = live ? c.mean[row] : 0.f, r.rstd = live ? c.rstd[row] : 0.f;
 #pragma unroll
     for (int k = 0; k < P; ++k) {
       const int ch = (k * L + l) * V, left = live ? c.C - ch : 0;
-      rx[k] = ry[k] = rt[k] = (Word4){0, 0, 0, 0};
+      r.x[k] = r.y[k] = r.t[k] = (Word4){0, 0, 0, 0};
       if (left <= 0) continue;
-      rx[k] = load_row<T>(at<T>(c.x, row, ch), left);
-      ry[k] = load_row<T>(at<T>(c.y, row, ch), left);
-      if (c.dtotal.p) rt[k] = load_row<T>(at<T>(c.dtotal, row, ch), left);
+      r.x[k] = load_row<T>(at<T>(c.x, row, ch), left);
+      r.y[k] = load_row<T>(at<T>(c.y, row, ch), left);
+      if (c.dtotal.p) r.t[k] = load_row<T>(at<T>(c.dtotal, row, ch), left);
     }
+  };
+  constexpr bool AHEAD = L < 1024;  // (1024 lanes have 128 registers each)
+  const int64_t step = (int64_t)gridDim.x * R;
+  int64_t first = (int64_t)blockIdx.x * R;
+  Row next;
+  if (AHEAD && first < c.rows) load(next, first + threadIdx.x / L);
+  for (; first < c.rows; first += step) {
+    const int64_t row = first + threadIdx.x / L;
+    if (!AHEAD) load(next, row);
+    const Row r = next;
+    if (AHEAD && first + step < c.rows) load(next, row + step);
     float s1 = 0.f, s2 = 0.f;
 #pragma unroll
     for (int k = 0; k < P; ++k) {
       float x[V], dy[V];
-      unpack_row<T>(rx[k], x);
-      unpack_row<T>(ry[k], dy);
+      unpack_row<T>(r.x[k], x);
+      unpack_row<T>(r.y[k], dy);
 #pragma unroll
       for (int i = 0; i < V; ++i) {
-        const float xh = (k * L + l) * V + i < c.C ? (x[i] - mean) * rstd : 0.f, t = dy[i] * w[k][i];
+        const float xh = (k * L + l) * V + i < c.C ? (x[i] - r.mean) * r.rstd : 0.f, t = dy[i] * w[k][i];
         s1 += t, s2 = fmaf(t, xh, s2);
         dw[k][i] = fmaf(dy[i], xh, dw[k][i]), db[k][i] += dy[i];
       }
     }
     row_sums<L>(s1, s2, turn);
     s1 *= over, s2 *= over;
+    if (row >= c.rows) continue;
 #pragma unroll
     for (int k = 0; k < P; ++k) {
-      const int ch = (k * L + l) * V, left = live ? c.C - ch : 0;
+      const int ch = (k * L + l) * V, left = c.C - ch;
       if (left <= 0) continue;
       float x[V], dy[V], dt[V], dx[V];
-      unpack_row<T>(rx[k], x);
-      unpack_row<T>(ry[k], dy);
-      unpack_row<T>(rt[k], dt);
+      unpack_row<T>(r.x[k], x);
+      unpack_row<T>(r.y[k], dy);
+      unpack_row<T>(r.t[k], dt);
 #pragma unroll
       for (int i = 0; i < V; ++i) {
-        const float xh = (x[i] - mean) * rstd;
-        dx[i] = fmaf(rstd, dy[i] * w[k][i] - s1 - xh * s2, dt[i]);
+        const float xh = (x[i] - r.mean) * r.rstd;
+        dx[i] = fmaf(r.rstd, dy[i] * w[k][i] - s1 - xh * s2, dt[i]);
       }
       store_row<T>(at<T>(c.dx, row, ch), left, pack_row<T>(dx));
     }
@@ -308,25 +323,26 @@ __global__ __launch_bounds__(kWide) void layer_norm_wide_backward_kernel(LayerNo
 struct Shape {
   int L, P;  // L = 0: wider than lanes hold
 };
-Shape shape_of(const LayerNormCall& c) {
+Shape shape_of(const LayerNormCall& c, bool backward) {
   if (c.C > kRegisterRow) return {0, 0};
   const int n = (int)cdiv(c.C, c.dtype == MDH_BF16 ? 8 : 4);
   if (n <= 8) return {8, 1};
   if (n <= 32) return {32, 1};
   if (n <= 64) return {64, 1};
   if (n <= 128) return {64, 2};
-  if (n <= 256) return {64, 4};
-  if (n <= 512) return {256, 2};
-  if (n <= 1024) return {256, 4};
+  // (backward a lane holds its weights and two sums besides: one piece each where that can be)
+  if (n <= 256) return backward ? Shape{256, 1} : Shape{64, 4};
+  if (n <= 512) return backward ? Shape{512, 1} : Shape{256, 2};
+  if (n <= 1024) return backward ? Shape{512, 2} : Shape{256, 4};
   if (n <= 2048) return {1024, 2};
-  return {1024, 4};
+  return backward ? Shape{0, 0} : Shape{1024, 4};
 }
-int64_t row_groups(const LayerNormCall& c) {  // workgroups that have a row
-  const Shape s = shape_of(c);
+int64_t row_groups(const LayerNormCall& c, bool backward) {  // workgroups that have a row
+  const Shape s = shape_of(c, backward);
   return s.L && s.L < 256 ? cdiv(c.rows, 256 / s.L) : c.rows;
 }
 int64_t backward_groups(const LayerNormCall& c) {
-  const int64_t n = row_groups(c);
+  const int64_t n = row_groups(c, true);
   return n < 512 ? n : 512;
 }
 
@@ -340,8 +356,8 @@ void go(const LayerNormCall& c, bool backward, unsigned blocks, hipStream_t st) 
 }
 template <typename T>
 mdh_status launch(const LayerNormCall& c, bool backward, hipStream_t st) {
-  const Shape s = shape_of(c);
-  const int64_t n = backward ? backward_groups(c) : row_groups(c);
+  const Shape s = shape_of(c, backward);
+  const int64_t n = backward ? backward_groups(c) : row_groups(c, false);
   if (n * (s.L == 0 || s.L > 256 ? 1024 : 256) >= (int64_t)1 << 32) return MDH_ERR_SIZE;
   const unsigned blocks = (unsigned)n;
   clear_stale_error();
@@ -350,12 +366,15 @@ mdh_status launch(const LayerNormCall& c, bool backward, hipStream_t st) {
     case 32 * 8 + 1: go<T, 32, 1>(c, backward, blocks, st); break;
     case 64 * 8 + 1: go<T, 64, 1>(c, backward, blocks, st); break;
     case 64 * 8 + 2: go<T, 64, 2>(c, backward, blocks, st); break;
-    case 64 * 8 + 4: go<T, 64, 4>(c, backward, blocks, st); break;
-    case 256 * 8 + 2: go<T, 256, 2>(c, backward, blocks, st); break;
-    case 256 * 8 + 4: go<T, 256, 4>(c, backward, blocks, st); break;
+    case 64 * 8 + 4: layer_norm_kernel<T, 64, 4><<<blocks, 256, 0, st>>>(c); break;
+    case 256 * 8 + 2: layer_norm_kernel<T, 256, 2><<<blocks, 256, 0, st>>>(c); break;
+    case 256 * 8 + 4: layer_norm_kernel<T, 256, 4><<<blocks, 256, 0, st>>>(c); break;
+    case 256 * 8 + 1: layer_norm_backward_kernel<T, 256, 1><<<blocks, 256, 0, st>>>(c); break;
+    case 512 * 8 + 1: layer_norm_backward_kernel<T, 512, 1><<<blocks, 512, 0, st>>>(c); break;
+    case 512 * 8 + 2: layer_norm_backward_kernel<T, 512, 2><<<blocks, 512, 0, st>>>(c); break;
     case 1024 * 8 + 2: go<T, 1024, 2>(c, backward, blocks, st); break;
     case 1024 * 8 + 4:
-      if constexpr (sizeof(T) == 4) go<T, 1024, 4>(c, backward, blocks, st);  // (bf16 rows of that many pieces are wide)
+      if constexpr (sizeof(T) == 4) layer_norm_kernel<T, 1024, 4><<<blocks, 1024, 0, st>>>(c);  // (bf16 rows of that many pieces are wide)
       break;
     default:
       if (backward)

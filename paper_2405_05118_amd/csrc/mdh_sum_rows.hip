@@ -1,11 +1,12 @@
 // Column sums of a matrix of fp32 partial results, in a fixed order: gradients of parameters, one row for each share of the
-// tokens.  Four teams of a workgroup take every fourth row of 64 columns, their sums are added in order.
+// tokens.  Sixteen teams of a workgroup take every sixteenth row of 64
+// columns, their sums are added in order.
 #include "mdh_internal.h"
 
 namespace mdh {
 namespace {
 
-constexpr int kTeams = 4;
+constexpr int kTeams = 16;
 
 struct SumArgs {
   const float* part;
@@ -29,7 +30,9 @@ __global__ __launch_bounds__(64 * kTeams) void sum_rows_kernel(SumArgs s) {
   sums[team][lane] = (x[0] + x[1]) + (x[2] + x[3]);
   __syncthreads();
   if (team || col >= s.n) return;
-  const float v = (sums[0][lane] + sums[1][lane]) + (sums[2][lane] + sums[3][lane]);
+  float v = 0.f;
+#pragma unroll
+  for (int k = 0; k < kTeams; ++k) v += sums[k][lane];
 #pragma unroll
   for (int i = 0; i < 3; ++i) {
     if (col >= 0 && col < s.to[i].n && s.to[i].p) s.to[i].p[col] = v;
