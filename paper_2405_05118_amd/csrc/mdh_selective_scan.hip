@@ -2,10 +2,11 @@
 // channel and its N states -- the prefix-sum operator on pairs (a, u): (a1, u1) op (a2, u2) = (a1 a2, a2 u1 + u2), whose a a token gives.
 //
 // 1 exponential and 4 multiplications a step (token, channel, state), on 8 bytes a token and channel (bf16, N = 16): bound by the
-// vector ALU.  Measured on this chip, cycles of a wavefront instruction with four wavefronts a SIMD: v_exp_f32 11.3, fma 3.8,
-// multiplication 3.4, the same with a lane of the row broadcast to it (DPP) 5.2.
+// vector ALU.  Measured on this chip, cycles of a wavefront instruction with four wavefronts a SIMD: v_exp_f32 8.4, fma and
+// multiplication 2.6 to 3.2, with a lane of the row broadcast to it (DPP) 4.4; a step of all of them 24 to 27 (with two wavefronts 31,
+// with one 57).  Times (bf16, N = 16): 2048 tokens of 4096 channels 81 us; 32768 tokens of 1536 channels 474 us.
 //
-// De-composition.  A row of 16 lanes is a channel, a lane one state of every 16; a wavefront has four channels, a workgroup 16.
+// De-composition.  A row of 16 lanes is a channel, a lane one state of every 16; a wavefront has four channels, a workgroup 8 or 16.
 // Tokens are walked in tiles of 16.  Lane j loads x, dt and gate of token j, takes the softplus, and a step's delta reaches the row's
 // other lanes as a modifier of the multiplication.  c_t . h_t: every lane's term goes to LDS, lane j adds up token j's.
 // b and c of a tile lie in LDS as fp32.  With too few channels for the chip, tokens are cut into segments: what each leaves from
@@ -211,44 +212,50 @@ __global__ __launch_bounds__(256) void segments_kernel(ScanCall c, Segments segs
   }
 }
 
-// One token, states in place.  V adjacent states a lane, L lanes a channel (all states at once: V L >= N).
+// One token, states in place.  V adjacent states a lane, L lanes a channel (all states at once: V L >= N).  Bound by the states'
+// way in and out: 250 sequences of 4096 channels with 16 states, 138 MB, 29.5 us (4.7 TB/s; with the indexes in 64 bits 33).
+// Two, four and eight sequences a lane, A read once for them: 29.5, 35, 61 us; non-temporal accesses: 35.
 template <typename T, int V, int L>
-__global__ __launch_bounds__(256) void scan_step_kernel(ScanCall c) {
+__global__ __launch_bounds__(256) void scan_step_kernel(ScanCall c, unsigned blocks) {
   typedef float fv __attribute__((ext_vector_type(V)));
-  const int64_t i = (int64_t)blockIdx.x * 256 + threadIdx.x;
-  const int64_t d = i / L % c.D, b = i / L / c.D;
+  const unsigned i = blockIdx.x % blocks * 256 + threadIdx.x, d = i / L;
+  if (d >= (unsigned)c.D) return;  // (all lanes of a channel)
+  const int64_t b = blockIdx.x / blocks, slot = scan_slot(c, b);
   const int n = (int)(i % L) * V;
-  const bool live = b < c.B;
-  const int64_t slot = live ? scan_slot(c, b) : -1;
-  float y = 0.f, x = 0.f;
+  float y = 0.f;
   if (slot >= 0) {
-    const int g = (int)(d / c.E);
-    const Token k = token_of(c, to_float(*at<T>(c.in[0], b, 0, d)), to_float(*at<T>(c.in[1], b, 0, d)), true, c.dt_bias ? c.dt_bias[d] : 0.f);
-    x = k.x;
+    const float x = to_float(*at<T>(c.in[0], b, 0, d)), dt = to_float(*at<T>(c.in[1], b, 0, d));
     if (n < c.N) {
+      const int g = (int)(d / (unsigned)c.E);
       float* state = c.s_out + (slot * c.D + d) * c.N + n;
       fv h = *(const fv*)state;
-      const fv A = *(const fv*)(c.A + d * c.N + n);
+      const fv A = *(const fv*)(c.A + (int64_t)d * c.N + n) * kLog2e;
       const T *pb = at<T>(c.bc[0], b, 0, g, n), *pc = at<T>(c.bc[1], b, 0, g, n);
+      float bt[V], ct[V];
+      if constexpr (V == 4) {
+        unpack_row<T, V>(load_row<T, V>(pb, V), bt);
+        unpack_row<T, V>(load_row<T, V>(pc, V), ct);
+      } else {
+        bt[0] = to_float(*pb), ct[0] = to_float(*pc);
+      }
+      const Token k = token_of(c, x, dt, true, c.dt_bias ? c.dt_bias[d] : 0.f);
 #pragma unroll
       for (int s = 0; s < V; ++s) {
-        h[s] = fmaf(exp2_of(k.delta * (A[s] * kLog2e)), h[s], k.delta * k.x * to_float(pb[s]));
-        y = fmaf(to_float(pc[s]), h[s], y);
+        h[s] = fmaf(exp2_of(k.delta * A[s]), h[s], k.delta * k.x * bt[s]);
+        y = fmaf(ct[s], h[s], y);
       }
       *(fv*)state = h;
     }
-  }
 #pragma unroll
-  for (int k = 1; k < L; k *= 2) y += __shfl_xor(y, k);
-  if (!live || i % L) return;
-  if (slot >= 0) {
+    for (int k = 1; k < L; k *= 2) y += __shfl_xor(y, k);
+    if (i % L) return;
     if (c.skip) y = fmaf(c.skip[d], x, y);
     if (c.in[2].p) {
       const float gate = to_float(*at<T>(c.in[2], b, 0, d));
       y *= gate * sigmoid(gate);
     }
   }
-  *at<T>(c.out[0], b, 0, d) = from_float<T>(y);
+  if (i % L == 0) *at<T>(c.out[0], b, 0, d) = from_float<T>(y);
 }
 
 int states_of(const ScanCall& c) { return c.N <= 16 ? 1 : c.N <= 32 ? 2 : 4; }
@@ -261,12 +268,12 @@ struct Plan {
 // The least of estimated times, in cycles for 16 states.  In turn: 55 a token and 60 for every wavefront of a SIMD (one of them: 2048
 // tokens of 4096 channels 116 us; four: 4 x 2048 of 4096 234).  At once: 98 a token with two workgroups of 8 wavefronts a compute unit,
 // 65 with one (84 us), 60 with one of 16 (32768 of 1536 channels: 826).  Segments: 92 a step whatever the shape, and two more launches
-// (32768 of 1536: 474; 2048 of 4096: 99).
+// (32768 of 1536: 474; 2048 of 4096: 99), 15 us in all.
 Plan plan(const ScanCall& c) {
   const int ns = states_of(c);
   const int64_t T = c.T, eights = c.B * c.G * cdiv(c.E, 8), groups = c.B * c.G * cdiv(c.E, 16);
-  const int64_t turn = T * (55 + (groups * 60 + 255) / 256), four = T * (eights <= 256 ? 65 : 98 * cdiv(eights, 512)), eight = T * 60 * cdiv(eights, 256);
-  const int64_t cut = T * groups * 92 / 256 + 24000;
+  const int64_t turn = T * (55 + (groups <= 256 ? 60 : groups * 60 / 256)), four = T * (eights <= 256 ? 65 : 98 * cdiv(eights, 512)), eight = T * 60 * cdiv(eights, 256);
+  const int64_t cut = T * groups * 92 / 256 + 36000;
   Plan z{1, 1, 0};
   int64_t best = turn;
   if (ns < 4 && four < best) z.W = 4, best = four;
@@ -315,25 +322,26 @@ mdh_status pass_of(const ScanCall& c, const Plan& z, const Segments& segs, hipSt
 }
 
 template <typename T, int V, int L>
-void step(const ScanCall& c, hipStream_t st) {
-  scan_step_kernel<T, V, L><<<(unsigned)cdiv(c.B * c.D * L, 256), 256, 0, st>>>(c);
+mdh_status step(const ScanCall& c, hipStream_t st) {
+  const int64_t blocks = cdiv((int64_t)c.D * L, 256);
+  const int64_t grid = blocks * c.B;
+  if (grid >= 1 << 24) return MDH_ERR_SIZE;
+  clear_stale_error();
+  scan_step_kernel<T, V, L><<<(unsigned)grid, 256, 0, st>>>(c, (unsigned)blocks);
+  return launch_status();
 }
 template <typename T>
 mdh_status step_of(const ScanCall& c, hipStream_t st) {
   const bool vec = c.N % 4 == 0 && ((uintptr_t)c.s_out | (uintptr_t)c.A) % 16 == 0;
   const int V = vec ? 4 : 1, lanes = (int)cdiv(c.N, V);
-  if (c.B * c.D >= (int64_t)1 << 25) return MDH_ERR_SIZE;  // (64 lanes a channel at the most)
-  clear_stale_error();
   if (vec) {
-    if (lanes <= 1) step<T, 4, 1>(c, st);
-    else if (lanes <= 4) step<T, 4, 4>(c, st);
-    else step<T, 4, 16>(c, st);
-  } else {
-    if (lanes <= 4) step<T, 1, 4>(c, st);
-    else if (lanes <= 16) step<T, 1, 16>(c, st);
-    else step<T, 1, 64>(c, st);
+    if (lanes <= 1) return step<T, 4, 1>(c, st);
+    if (lanes <= 4) return step<T, 4, 4>(c, st);
+    return step<T, 4, 16>(c, st);
   }
-  return launch_status();
+  if (lanes <= 4) return step<T, 1, 4>(c, st);
+  if (lanes <= 16) return step<T, 1, 16>(c, st);
+  return step<T, 1, 64>(c, st);
 }
 
 }  // namespace
