@@ -242,12 +242,20 @@ __device__ __forceinline__ float row_sum(const float* lds, int lane) {
   const f4 s = (p[0] + p[1]) + (p[2] + p[3]);
   return (s[0] + s[1]) + (s[2] + s[3]);
 }
-// The same values summed over the four rows of a wavefront: lane (r, j) those of lanes j for tokens 4 r + 0 .. 3
-__device__ __forceinline__ Float4 over_rows(const float* lds, int lane) {
-  const float* p = lds + (lane >> 4) * 4 * kSumPitch + (lane & 15);
+// A lane's 16 values, of a token each, summed over the four rows of a wavefront: lane (r, j) those of lanes j for tokens 4 r + 0 .. 3
+__device__ __forceinline__ Float4 over_rows(const float (&v)[kTile]) {
+  float half[8];
   Float4 s;
 #pragma unroll
-  for (int i = 0; i < 4; ++i) s[i] = (p[i * kSumPitch] + p[i * kSumPitch + 16]) + (p[i * kSumPitch + 32] + p[i * kSumPitch + 48]);
+  for (int t = 0; t < 8; ++t) {
+    const auto x = __builtin_amdgcn_permlane32_swap(__float_as_uint(v[t]), __float_as_uint(v[t + 8]), false, false);
+    half[t] = __uint_as_float(x[0]) + __uint_as_float(x[1]);  // rows 0 and 1: token t, 2 and 3: t + 8
+  }
+#pragma unroll
+  for (int t = 0; t < 4; ++t) {
+    const auto x = __builtin_amdgcn_permlane16_swap(__float_as_uint(half[t]), __float_as_uint(half[t + 4]), false, false);
+    s[t] = __uint_as_float(x[0]) + __uint_as_float(x[1]);
+  }
   return s;
 }
 // between a wavefront's stores to LDS and other lanes' loads of them, and back

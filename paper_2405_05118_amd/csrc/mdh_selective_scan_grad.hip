@@ -96,7 +96,7 @@ __global__ __launch_bounds__(64 * WAVES, NS == 1 && sizeof(T) == 2 ? 4 : 2) void
   typedef Stage<T, 4, 2, CH, S, kTokens, THREADS> In;
   typedef Outputs<T, 3, CH, kTokens, THREADS> Out;
   __shared__ T raw[4 * kTokens * CH] __attribute__((aligned(16)));
-  __shared__ float bc[2 * In::kFloats] __attribute__((aligned(16))), sums[WAVES][kSumFloats] __attribute__((aligned(16)));
+  __shared__ float bc[2 * In::kFloats] __attribute__((aligned(16))), sums[WAVES][kSumFloats] __attribute__((aligned(16))), meet[2][WAVES][512];
   T *const xs = raw, *const dts = raw + kTokens * CH, *const gates = raw + 2 * kTokens * CH, *const dys = raw + 3 * kTokens * CH;
   const ScanPlace p = scan_place(c, blocks, w.n, w.tokens);
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
@@ -136,6 +136,7 @@ __global__ __launch_bounds__(64 * WAVES, NS == 1 && sizeof(T) == 2 ? 4 : 2) void
     if (c.out[i].p) store_zeros<T, CH, THREADS>(c.out[i], p, d0, width, kTokens);
   Out out;
   out.begin(c.out, p, t0, -1, d0, width);
+  int turn = 0;
   bool behind = false;  // a block's gradients lie in LDS
   for (; t0 >= p.first; t0 -= kTokens) {
     if (behind) out.take(raw);
@@ -181,13 +182,18 @@ __global__ __launch_bounds__(64 * WAVES, NS == 1 && sizeof(T) == 2 ? 4 : 2) void
         settle(sp);
         wave_fence();
         const float dp2 = again(dp), delta2 = again(k.delta), u2 = again(u);
+        float terms[kTile];
         unroll<kTile>([&](auto i) {
           constexpr int I = decltype(i)::value;
-          own[I * kSumPitch + lane] = lane_of_row<I>(dp) * h[I + 1];
+          terms[I] = lane_of_row<I>(dp) * h[I + 1];
         });
-        wave_fence();
-        const Float4 dc = over_rows(own, lane);
-        wave_fence();
+        Float4 dc = over_rows(terms);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          float v = dc[i];
+          settle(v);
+          dc[i] = v;
+        }
         unroll<kTile / 4>([&](auto quarter) {
           constexpr int Q = kTile - 4 - decltype(quarter)::value * 4;
           const Float4 bt = four_of(bs + Q), ct = four_of(bs + In::kFloats + Q);
@@ -206,11 +212,9 @@ __global__ __launch_bounds__(64 * WAVES, NS == 1 && sizeof(T) == 2 ? 4 : 2) void
         wave_fence();
         unroll<kTile>([&](auto i) {
           constexpr int I = decltype(i)::value;
-          own[I * kSumPitch + lane] = lane_of_row<I>(u2) * g[I];
+          g[I] *= lane_of_row<I>(u2);
         });
-        wave_fence();
-        const Float4 db = over_rows(own, lane);
-        wave_fence();
+        const Float4 db = over_rows(g);
 #pragma unroll
         for (int i = 0; i < kTile; ++i) own[i * kSumPitch + lane] = a[i] * A[s];
         wave_fence();
@@ -219,18 +223,18 @@ __global__ __launch_bounds__(64 * WAVES, NS == 1 && sizeof(T) == 2 ? 4 : 2) void
         wave_fence();
         // over the wavefronts
 #pragma unroll
-        for (int i = 0; i < 4; ++i) own[i * 64 + lane] = db[i], own[256 + i * 64 + lane] = dc[i];
+        for (int i = 0; i < 4; ++i) meet[turn][wave][i * 64 + lane] = db[i], meet[turn][wave][256 + i * 64 + lane] = dc[i];
         __syncthreads();
 #pragma unroll
         for (int i = threadIdx.x; i < 512; i += THREADS) {
           const int which = i / 256, t = i / 16 % 4 * 4 + i / 64 % 4, n = s * 16 + i % 16;
-          float sum = sums[0][i];
+          float sum = meet[turn][0][i];
 #pragma unroll
-          for (int v = 1; v < WAVES; ++v) sum += sums[v][i];
+          for (int v = 1; v < WAVES; ++v) sum += meet[turn][v][i];
           if (n < c.N && i0 + t < tokens)
             w.shared[(((which * (int64_t)blocks + p.block) * c.B + p.b) * c.T + t0 + i0 + t) * c.G * c.N + (int64_t)p.g * c.N + n] = sum;
         }
-        __syncthreads();
+        turn ^= 1;  // (whoever writes there again has been past another barrier)
       }
       const float d_delta = fmaf(k.x, sr, sq * kLn2), d_dt = c.softplus ? d_delta * sigmoid(k.raw) : d_delta;
       d_skip = fmaf(dp, k.x, d_skip);
