@@ -136,6 +136,11 @@ __global__ __launch_bounds__(64 * WAVES, NS == 1 && sizeof(T) == 2 ? 4 : 2) void
     if (c.out[i].p) store_zeros<T, CH, THREADS>(c.out[i], p, d0, width, kTokens);
   Out out;
   out.begin(c.out, p, t0, -1, d0, width);
+  // of the 512 sums of a tile (d_b and d_c of 16 tokens and 16 states) a thread adds up its own over the wavefronts
+  static_assert(THREADS == 512, "a thread's sum of d_b or d_c");
+  const int shared_t = (int)threadIdx.x / 16 % 4 * 4 + (int)threadIdx.x / 64 % 4, shared_n = p.j, per_token = c.G * c.N;
+  const int shared_at = shared_t * per_token + shared_n, which = __builtin_amdgcn_readfirstlane((int)threadIdx.x / 256);
+  float* const shared_to = w.shared + ((which * (int64_t)blocks + p.block) * c.B + p.b) * c.T * per_token + (int64_t)p.g * c.N;
   int turn = 0;
   bool behind = false;  // a block's gradients lie in LDS
   for (; t0 >= p.first; t0 -= kTokens) {
@@ -225,15 +230,10 @@ __global__ __launch_bounds__(64 * WAVES, NS == 1 && sizeof(T) == 2 ? 4 : 2) void
 #pragma unroll
         for (int i = 0; i < 4; ++i) meet[turn][wave][i * 64 + lane] = db[i], meet[turn][wave][256 + i * 64 + lane] = dc[i];
         __syncthreads();
+        float sum = meet[turn][0][threadIdx.x];
 #pragma unroll
-        for (int i = threadIdx.x; i < 512; i += THREADS) {
-          const int which = i / 256, t = i / 16 % 4 * 4 + i / 64 % 4, n = s * 16 + i % 16;
-          float sum = meet[turn][0][i];
-#pragma unroll
-          for (int v = 1; v < WAVES; ++v) sum += meet[turn][v][i];
-          if (n < c.N && i0 + t < tokens)
-            w.shared[(((which * (int64_t)blocks + p.block) * c.B + p.b) * c.T + t0 + i0 + t) * c.G * c.N + (int64_t)p.g * c.N + n] = sum;
-        }
+        for (int v = 1; v < WAVES; ++v) sum += meet[turn][v][threadIdx.x];
+        if (s * 16 + shared_n < c.N && i0 + shared_t < tokens) (shared_to + (t0 + i0) * per_token + s * 16)[shared_at] = sum;
         turn ^= 1;  // (whoever writes there again has been past another barrier)
       }
       const float d_delta = fmaf(k.x, sr, sq * kLn2), d_dt = c.softplus ? d_delta * sigmoid(k.raw) : d_delta;
