@@ -27,6 +27,12 @@ template <int J>
 __device__ __forceinline__ float lane_of_row(float v) {
   return __int_as_float(__builtin_amdgcn_mov_dpp(__float_as_int(v), 0x150 + J, 0xf, 0xf, true));
 }
+// lane J's value of `v` times x, added to sum.  (The compiler broadcasts to a register first; the two wait states are those between
+// an instruction that writes a register and a broadcast of it.)
+template <int J>
+__device__ __forceinline__ void add_lane_of_row(float& sum, float v, float x) {
+  asm("s_nop 1\n\tv_fmac_f32_dpp %0, %1, %2 row_newbcast:%3 row_mask:0xf bank_mask:0xf" : "+v"(sum) : "v"(v), "v"(x), "n"(J));
+}
 // computed here, not behind the next barrier with all that it is computed from in registers until there
 __device__ __forceinline__ void settle(float& v) { asm volatile("" : "+v"(v)); }
 // The same value to be broadcast at another place: where the compiler knows that two broadcasts are one, it keeps their result in
@@ -37,6 +43,15 @@ __device__ __forceinline__ float again(float v) {
 }
 // 2^x by the hardware (1 ulp; 0 below 2^-126)
 __device__ __forceinline__ float exp2_of(float x) { return __builtin_amdgcn_exp2f(x); }
+
+// The factor 2^(delta A) of a state.  v_exp_f32 is too small by 0.12 2^-24 on average where its result is just below 1 (a million
+// arguments from -1e-2 to -1e-5; no more than 0.7 2^-24 at any), which a state that decays slowly adds up over its thousands of tokens:
+// 1e-8 more in the exponent (2^0 stays 1) takes final states and gradients of 1001 tokens from 1.9e-6 to 8e-7 off.  One more instruction
+// where delta is broadcast; left out for bf16, whose operands are off by 2^-9.
+template <typename T>
+__device__ __forceinline__ float factor_of(float delta, float A) {
+  return exp2_of(sizeof(T) == 4 ? fmaf(delta, A, 1e-8f) : delta * A);
+}
 
 // e^v with the rounding of v log2(e) put right
 __device__ __forceinline__ float exp_of(float v) {

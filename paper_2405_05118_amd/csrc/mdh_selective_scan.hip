@@ -50,7 +50,7 @@ __global__ __launch_bounds__(F::THREADS) void scan_kernel(ScanCall c, Segments s
   __shared__ float2 ends[W > 1 ? W : 1][W > 1 ? CH * S : 1];
   T *const xs = raw, *const dts = raw + TOKENS * CH, *const gates = raw + 2 * TOKENS * CH;
   ScanPlace p = scan_place(c, blocks, segs.n, segs.tokens);
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, tile = p.row / CH;
+  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, tile = W > 1 ? __builtin_amdgcn_readfirstlane(p.row / CH) : 0;
   p.row %= CH;
   const int e0 = p.block * CH, width = min(CH, c.E - e0);
   const bool mine = p.row < width;
@@ -77,11 +77,13 @@ __global__ __launch_bounds__(F::THREADS) void scan_kernel(ScanCall c, Segments s
     skip = c.skip ? c.skip[d] : 0.f;
     dt_bias = c.dt_bias ? c.dt_bias[d] : 0.f;
   }
+  const int64_t all_states = (int64_t)c.D * c.N, state_at = d * c.N + p.j;
   auto keep = [&](int64_t t, const float (&state)[NS]) {
     if (STATES_ONLY || !c.checkpoints || t >= p.alive) return;
+    float* to = c.checkpoints + (p.b * c.tiles + t / kTile) * all_states;  // (the same for the wavefront)
 #pragma unroll
     for (int s = 0; s < NS; ++s)
-      if (mine && s * 16 + p.j < c.N) c.checkpoints[((p.b * c.tiles + t / kTile) * c.D + d) * c.N + s * 16 + p.j] = state[s];
+      if (mine && s * 16 + p.j < c.N) (to + s * 16)[state_at] = state[s];
   };
   Out out;
   if (!STATES_ONLY) out.begin(c.out, p, p.first, 1, d0, width);
@@ -110,7 +112,7 @@ __global__ __launch_bounds__(F::THREADS) void scan_kernel(ScanCall c, Segments s
             const Float4 bt = four_of(bs + s * 16 * In::kPitch + Q), ct = four_of(bs + (STATES_ONLY ? 0 : In::kFloats) + s * 16 * In::kPitch + Q);
             unroll<4>([&](auto i) {
               constexpr int I = decltype(i)::value;
-              const float a = exp2_of(lane_of_row<Q + I>(k.delta) * A[s]);
+              const float a = factor_of<T>(lane_of_row<Q + I>(k.delta), A[s]);
               h[s] = fmaf(a, h[s], lane_of_row<Q + I>(u) * bt[I]);
               if (!STATES_ONLY) y[Q + I] = s ? fmaf(ct[I], h[s], y[Q + I]) : ct[I] * h[s];
             });
@@ -125,7 +127,7 @@ __global__ __launch_bounds__(F::THREADS) void scan_kernel(ScanCall c, Segments s
             const Float4 bt = four_of(bs + s * 16 * In::kPitch + Q);
             unroll<4>([&](auto i) {
               constexpr int I = decltype(i)::value;
-              const float a = exp2_of(lane_of_row<Q + I>(k.delta) * A[s]);
+              const float a = factor_of<T>(lane_of_row<Q + I>(k.delta), A[s]);
               from_zero = fmaf(a, from_zero, lane_of_row<Q + I>(u) * bt[I]);
               all *= a;
               own[s][Q + I] = from_zero, product[s][Q + I] = all;
@@ -241,7 +243,7 @@ __global__ __launch_bounds__(256) void scan_step_kernel(ScanCall c, unsigned blo
       const Token k = token_of(c, x, dt, true, c.dt_bias ? c.dt_bias[d] : 0.f);
 #pragma unroll
       for (int s = 0; s < V; ++s) {
-        h[s] = fmaf(exp2_of(k.delta * A[s]), h[s], k.delta * k.x * bt[s]);
+        h[s] = fmaf(factor_of<float>(k.delta, A[s]), h[s], k.delta * k.x * bt[s]);
         y = fmaf(ct[s], h[s], y);
       }
       *(fv*)state = h;

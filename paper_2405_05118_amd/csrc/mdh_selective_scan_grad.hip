@@ -73,7 +73,7 @@ __global__ __launch_bounds__(kThreads) void grad_segments_kernel(ScanCall c, Par
           const Float4 ct = four_of(cs + (s * 16 + p.j) * In::kPitch + i0 + Q);
           unroll<4>([&](auto i) {
             constexpr int I = 3 - decltype(i)::value;
-            e[s] = exp2_of(lane_of_row<Q + I>(k.delta) * A[s]) * fmaf(lane_of_row<Q + I>(dp), ct[I], e[s]);
+            e[s] = factor_of<T>(lane_of_row<Q + I>(k.delta), A[s]) * fmaf(lane_of_row<Q + I>(dp), ct[I], e[s]);
           });
         });
     }
@@ -108,6 +108,7 @@ __global__ __launch_bounds__(64 * WAVES, NS == 1 && sizeof(T) == 2 ? 4 : 2) void
   int64_t t0 = last_block(p, kTokens);
   in.begin(c.in, c.bc, p, t0, -1, d0, width, c.N);
   float A[NS], e[NS], dA[NS], next_h[TILES][NS], d_skip = 0.f, d_bias = 0.f;
+  const int64_t all_states = (int64_t)c.D * c.N, state_at = d * c.N + p.j;
   auto load = [&](int64_t from) {
     in.load(p.alive - from);
 #pragma unroll
@@ -116,7 +117,7 @@ __global__ __launch_bounds__(64 * WAVES, NS == 1 && sizeof(T) == 2 ? 4 : 2) void
       for (int s = 0; s < NS; ++s) {
         next_h[i][s] = 0.f;
         if (mine && s * 16 + p.j < c.N && from + i * kTile < p.alive)
-          next_h[i][s] = c.checkpoints[((p.b * c.tiles + from / kTile + i) * c.D + d) * c.N + s * 16 + p.j];
+          next_h[i][s] = (c.checkpoints + (p.b * c.tiles + from / kTile + i) * all_states + s * 16)[state_at];
       }
   };
   if (t0 >= p.first) load(t0);
@@ -177,7 +178,7 @@ __global__ __launch_bounds__(64 * WAVES, NS == 1 && sizeof(T) == 2 ? 4 : 2) void
           const Float4 bt = four_of(bs + Q), ct = four_of(bs + In::kFloats + Q);
           unroll<4>([&](auto i) {
             constexpr int I = Q + decltype(i)::value;
-            a[I] = exp2_of(lane_of_row<I>(k.delta) * A[s]);
+            a[I] = factor_of<T>(lane_of_row<I>(k.delta), A[s]);
             h[I + 1] = fmaf(a[I], h[I], lane_of_row<I>(u) * bt[I - Q]);
             own[I * kSumPitch + lane] = ct[I - Q] * h[I + 1];
           });
@@ -204,11 +205,12 @@ __global__ __launch_bounds__(64 * WAVES, NS == 1 && sizeof(T) == 2 ? 4 : 2) void
           const Float4 bt = four_of(bs + Q), ct = four_of(bs + In::kFloats + Q);
           unroll<4>([&](auto i) {
             constexpr int I = Q + 3 - decltype(i)::value;
-            g[I] = fmaf(lane_of_row<I>(dp2), ct[I - Q], e[s]);
+            g[I] = e[s];
+            add_lane_of_row<I>(g[I], dp2, ct[I - Q]);
             own[I * kSumPitch + lane] = g[I] * bt[I - Q];
             e[s] = a[I] * g[I];
             a[I] = e[s] * h[I];  // (the factor is done with)
-            dA[s] = fmaf(lane_of_row<I>(delta2), a[I], dA[s]);
+            add_lane_of_row<I>(dA[s], delta2, a[I]);
           });
         });
         wave_fence();

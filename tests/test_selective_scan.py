@@ -175,6 +175,33 @@ def test_long_sequences(dtype, B, T, D, N, G):
 
 
 @gpu
+@pytest.mark.parametrize("B,T,D,N", [(1, 16384, 16, 16), (1, 16000, 4096, 16), (4, 8192, 4096, 8), (1, 9000, 4, 40)])
+def test_slow_decays_add_up_no_bias(B, T, D, N):
+    """Time steps of about 2^-13 that differ from token to token (with one for all of them a factor's rounding would be the same each time,
+    up to T u / 2 in all): h_T = sum of delta_t a^(T-t), the gradient of what it began with a^T, the same for every channel.
+    Factors and states are each rounded with half a step or so of random sign: 0.5 u of a token, sqrt(T / N) of that in the mean over N
+    states, four times which are allowed.  What is of one sign adds up: less than a sixteenth of a step, T u / 16.  32 u for the rest."""
+    delta = torch.rand(T, generator=torch.Generator().manual_seed(1)) * 2.0 ** -13 + 2.0 ** -14
+    A = (-1 - torch.arange(N) / 16.0).expand(D, N).contiguous().cuda()
+    x, dt = torch.ones(B, T, D, device="cuda"), delta.cuda()[None, :, None].expand(B, T, D).contiguous()
+    b, c = torch.ones(B, T, 1, N, device="cuda"), torch.zeros(B, T, 1, N, device="cuda")
+    y, end, begin = torch.empty_like(x), torch.empty(B, D, N, device="cuda"), torch.empty(B, D, N, device="cuda")
+    sizes = (B, T, D, N, 1)
+    kept = torch.empty(mdh.mdh_selective_scan_checkpoints_size(sizes), dtype=torch.uint8, device="cuda")
+    ws = torch.empty(mdh.mdh_selective_scan_workspace_size(sizes, F32, True), dtype=torch.uint8, device="cuda")
+    mdh.mdh_selective_scan(x, dt, A, b, c, y, final_state=end, checkpoints=kept, workspace=ws)
+    d_x, d_dt, d_b, d_c = (torch.empty_like(v) for v in (x, dt, b, c))
+    mdh.mdh_selective_scan_backward(x, dt, A, b, c, 0 * x, d_x, d_dt, torch.empty_like(A), d_b, d_c, kept, d_final_state=torch.ones_like(end),
+                                    d_initial_state=begin, workspace=ws)
+    steps = np64(delta)
+    after = steps.sum() - np.cumsum(steps)  # behind each token
+    refs = np.exp(np.outer(after, np64(A)[0])).T @ steps, np.exp(np64(A)[0] * steps.sum())
+    for got, ref, what in zip((end, begin), refs, ("end", "begin")):
+        off = float(np.abs((np64(got) / ref - 1).mean(axis=-1)).max()) / U
+        assert off <= T / 16 + 2 * np.sqrt(T / N) + 32, "%s: %.0f" % (what, off)
+
+
+@gpu
 @pytest.mark.parametrize("dtype", [F32, BF16])
 def test_strides(dtype):
     """Columns of one projection, at odd places; tokens before batch entries; one token's values for all tokens."""
