@@ -603,7 +603,7 @@ mdh_status mdh_group_norm_backward(const int64_t* sizes, mdh_dtype dtype, const 
  * X_t the token t of x, and for t < 0 row W - 1 + t of the window that came in (zeros without one):
  * md_hom(*, (++, ++, ++, +)) over (b, t, ch, j), mdh_mcc's index function t + j with no dimension over channels.
  *   sizes    (B, T, C, W): 0 <= B, 0 <= T < 2^31 - 64, B * T < 2^31, 1 <= C < 2^24, 1 <= W <= 8 (MDH_ERR_UNSUPPORTED).
- *            A call has fewer than 2^32 - 256 lanes (MDH_ERR_SIZE), one for 16 bytes of the channels of 8 to 64 tokens.
+ *            A call has fewer than 2^24 workgroups of 256 lanes (MDH_ERR_SIZE), a lane for 4 channels of 8 to 64 tokens.
  *   x, y     (B, T, C) of type dtype; strides: 4 numbers, (batch, token) of x, y in elements, channels adjacent;
  *            NULL: dense.  Any alignment that the type has.  y does not overlap x.
  *   weight   (C, W) fp32; bias: C fp32 or NULL (zeros); act: MDH_ACT_*
@@ -649,13 +649,15 @@ mdh_status mdh_causal_conv_step(const int64_t* sizes, mdh_dtype dtype, const voi
  * -- the prefix-sum operator on pairs, (a1, u1) op (a2, u2) = (a1 a2, a2 u1 + u2) (paper: Appendix, Example "Prefix-Sum"), with a
  * factor that every token gives, where mdh_linattn's is a constant of the head.
  *   sizes    (B, T, D, N, G): 0 <= B, 0 <= T < 2^31 - 64, B * T < 2^31, 1 <= D < 2^24, 1 <= N <= 64 (MDH_ERR_UNSUPPORTED), G divides
- *            D, B * T * G * N < 2^32.  A call has fewer than 2^24 workgroups, backward 2^23 (MDH_ERR_SIZE): one for each 16
- *            (backward: 64) channels of a group and batch entry.
+ *            D, B * T * G * N < 2^32.  A call has fewer than 2^22 workgroups (backward 2^23): one, or one for each segment of the
+ *            tokens, for 8 or 16 (backward: 32) channels of a group and batch entry; B * D * N < 2^32 where there are segments
+ *            (MDH_ERR_SIZE).
  *   x, dt, gate, y  (B, T, D) of type dtype; gate: NULL = no gate.  b, c: (B, T, G, N).
  *   strides  14 numbers: (batch, token) of x, dt, gate, y, then (batch, token, group) of b, c, in elements; channels and
  *            states are adjacent; NULL: all dense.  Inputs may have stride 0.  Any alignment that the type has.  y may be dt
  *            or gate (the same elements), and overlaps no other input.
- *   A        (D, N) fp32, finite; skip, dt_bias: D fp32 or NULL (zeros)
+ *   A        (D, N) fp32, finite; delta A is not above 0 (the factors of several tokens are multiplied before the state is: their
+ *            product may overflow where the states would not).  skip, dt_bias: D fp32 or NULL (zeros)
  *   lengths  as of mdh_causal_conv
  *   initial_state, final_state  (B, D, N) fp32; NULL: zeros / not wanted.  They may be the same buffer.  With slots pools of
  *            n_slots states, as of mdh_causal_conv.

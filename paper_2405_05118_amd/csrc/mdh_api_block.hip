@@ -31,10 +31,11 @@ SharedView shared(const void* p, const int64_t* strides, const ScanCall& c) {
   if (c.G == 1) v.sg = 0;
   return v;
 }
-// an output whose elements share a place has no value
-bool overlaps(const TokenView& v, int64_t B, int64_t T) { return (B > 1 && T > 0 && v.sb == 0) || (T > 1 && v.st == 0); }
+// an output whose elements share a place has no value: rows of n elements closer than that
+bool closer(int64_t extent, int64_t stride, int64_t n) { return extent > 1 && (stride < 0 ? -stride : stride) < n; }
+bool overlaps(const TokenView& v, int64_t B, int64_t T, int64_t C) { return T > 0 && (closer(B, v.sb, C) || closer(T, v.st, C)); }
 bool overlaps(const SharedView& v, const ScanCall& c) {
-  return (c.B > 1 && c.T > 0 && v.sb == 0) || (c.T > 1 && v.st == 0) || (c.G > 1 && c.T > 0 && v.sg == 0);
+  return c.T > 0 && (closer(c.B, v.sb, c.N) || closer(c.T, v.st, c.N) || closer(c.G, v.sg, c.N));
 }
 
 // (B, T, C, W), without T for one token
@@ -89,7 +90,7 @@ mdh_status mdh_causal_conv(const int64_t* sizes, mdh_dtype dtype, const void* x,
   if (!weight || (c.T > 0 && (!x || !y))) return MDH_ERR_NULL;
   if (any_misaligned(bytes_of(dtype), x, y, initial_window, final_window) || any_misaligned(4, weight, bias)) return MDH_ERR_UNSUPPORTED;
   c.x = tokens(x, strides, c.B, c.T, c.C), c.y = tokens(y, strides ? strides + 2 : nullptr, c.B, c.T, c.C);
-  if (overlaps(c.y, c.B, c.T)) return MDH_ERR_SIZE;
+  if (overlaps(c.y, c.B, c.T, c.C)) return MDH_ERR_SIZE;
   c.weight = weight, c.bias = bias, c.lengths = lengths, c.slots = slots, c.n_slots = n_slots;
   c.s_in = initial_window, c.s_out = final_window;
   return launch_conv(c, (hipStream_t)stream);
@@ -114,7 +115,7 @@ mdh_status mdh_causal_conv_backward(const int64_t* sizes, mdh_dtype dtype, const
   if (short_of(workspace, workspace_bytes, conv_workspace(c))) return MDH_ERR_WORKSPACE;
   auto view = [&](const void* p, int i) { return tokens(p, strides ? strides + 2 * i : nullptr, c.B, c.T, c.C); };
   c.x = view(x, 0), c.y = view(d_y, 1), c.dx = view(d_x, 2);
-  if (overlaps(c.dx, c.B, c.T)) return MDH_ERR_SIZE;
+  if (overlaps(c.dx, c.B, c.T, c.C)) return MDH_ERR_SIZE;
   c.weight = weight, c.bias = bias, c.lengths = lengths, c.s_in = initial_window, c.d_out = d_final_window, c.d_in = d_initial_window;
   c.part = (float*)workspace, c.dweight = d_weight, c.dbias = d_bias;
   return launch_conv_backward(c, (hipStream_t)stream);
@@ -132,7 +133,7 @@ mdh_status mdh_causal_conv_step(const int64_t* sizes, mdh_dtype dtype, const voi
   if (any_misaligned(bytes_of(dtype), x, y, window) || any_misaligned(4, weight, bias)) return MDH_ERR_UNSUPPORTED;
   const int64_t sx[2] = {strides ? strides[0] : c.C, 0}, sy[2] = {strides ? strides[1] : c.C, 0};
   c.x = tokens(x, sx, c.B, 1, c.C), c.y = tokens(y, sy, c.B, 1, c.C);
-  if (overlaps(c.y, c.B, 1)) return MDH_ERR_SIZE;
+  if (overlaps(c.y, c.B, 1, c.C)) return MDH_ERR_SIZE;
   c.weight = weight, c.bias = bias, c.slots = slots, c.n_slots = n_slots, c.s_out = window;
   return launch_conv_step(c, (hipStream_t)stream);
 }
@@ -167,7 +168,7 @@ mdh_status mdh_selective_scan(const int64_t* sizes, mdh_dtype dtype, const void*
   auto view = [&](const void* p, int i) { return tokens(p, strides ? strides + 2 * i : nullptr, c.B, c.T, c.D); };
   c.in[0] = view(x, 0), c.in[1] = view(dt, 1), c.in[2] = view(gate, 2), c.out[0] = view(y, 3);
   c.bc[0] = shared(b, strides ? strides + 8 : nullptr, c), c.bc[1] = shared(c_, strides ? strides + 11 : nullptr, c);
-  if (overlaps(c.out[0], c.B, c.T)) return MDH_ERR_SIZE;
+  if (overlaps(c.out[0], c.B, c.T, c.D)) return MDH_ERR_SIZE;
   c.A = A, c.skip = skip, c.dt_bias = dt_bias, c.softplus = softplus != 0, c.lengths = lengths, c.slots = slots, c.n_slots = n_slots;
   c.s_in = initial_state, c.s_out = final_state, c.checkpoints = (float*)checkpoints, c.ws = workspace;
   return launch_scan_forward(c, (hipStream_t)stream);
@@ -196,7 +197,7 @@ mdh_status mdh_selective_scan_backward(const int64_t* sizes, mdh_dtype dtype, co
   c.out[0] = view(d_x, 4), c.out[1] = view(d_dt, 5), c.out[2] = view(gate ? d_gate : nullptr, 6);
   c.bc[0] = view2(b, 0), c.bc[1] = view2(c_, 1), c.dbc[0] = view2(d_b, 2), c.dbc[1] = view2(d_c, 3);
   for (int i = 0; i < (gate ? 3 : 2); ++i)
-    if (overlaps(c.out[i], c.B, c.T)) return MDH_ERR_SIZE;
+    if (overlaps(c.out[i], c.B, c.T, c.D)) return MDH_ERR_SIZE;
   if (overlaps(c.dbc[0], c) || overlaps(c.dbc[1], c)) return MDH_ERR_SIZE;
   c.A = A, c.skip = skip, c.dt_bias = dt_bias, c.softplus = softplus != 0, c.lengths = lengths;
   c.s_in = d_final_state, c.s_out = d_initial_state, c.checkpoints = (float*)checkpoints, c.ws = workspace;
@@ -225,7 +226,7 @@ mdh_status mdh_selective_scan_step(const int64_t* sizes, mdh_dtype dtype, const 
   };
   c.in[0] = view(x, 0), c.in[1] = view(dt, 1), c.in[2] = view(gate, 2), c.out[0] = view(y, 3);
   c.bc[0] = view2(b, 0), c.bc[1] = view2(c_, 1);
-  if (overlaps(c.out[0], c.B, 1)) return MDH_ERR_SIZE;
+  if (overlaps(c.out[0], c.B, 1, c.D)) return MDH_ERR_SIZE;
   c.A = A, c.skip = skip, c.dt_bias = dt_bias, c.softplus = softplus != 0, c.slots = slots, c.n_slots = n_slots, c.s_out = state;
   return launch_scan_step(c, (hipStream_t)stream);
 }

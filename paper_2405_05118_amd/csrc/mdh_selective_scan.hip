@@ -215,14 +215,17 @@ __global__ __launch_bounds__(256) void segments_kernel(ScanCall c, Segments segs
 }
 
 // One token, states in place.  V adjacent states a lane, L lanes a channel (all states at once: V L >= N).  Bound by the states'
-// way in and out: 250 sequences of 4096 channels with 16 states, 138 MB, 29.5 us (4.7 TB/s; with the indexes in 64 bits 33).
+// way in and out: 250 sequences of 4096 channels with 16 states, 138 MB, 29 us (4.8 TB/s; with the indexes in 64 bits 33).
 // Two, four and eight sequences a lane, A read once for them: 29.5, 35, 61 us; non-temporal accesses: 35.
-template <typename T, int V, int L>
+// ROWS: a workgroup is of one sequence, `blocks` of them each (else lanes go over sequences: a division for each lane, 31 us).
+template <typename T, int V, int L, bool ROWS>
 __global__ __launch_bounds__(256) void scan_step_kernel(ScanCall c, unsigned blocks) {
   typedef float fv __attribute__((ext_vector_type(V)));
-  const unsigned i = blockIdx.x % blocks * 256 + threadIdx.x, d = i / L;
-  if (d >= (unsigned)c.D) return;  // (all lanes of a channel)
-  const int64_t b = blockIdx.x / blocks, slot = scan_slot(c, b);
+  const unsigned row = ROWS ? blockIdx.x / blocks : 0, i = (blockIdx.x - row * blocks) * 256 + threadIdx.x;
+  const unsigned at_b = ROWS ? row : i / L / (unsigned)c.D, d = ROWS ? i / L : i / L - at_b * (unsigned)c.D;
+  const int64_t b = at_b;
+  if (b >= c.B || d >= (unsigned)c.D) return;  // (all lanes of a channel)
+  const int64_t slot = scan_slot(c, b);
   const int n = (int)(i % L) * V;
   float y = 0.f;
   if (slot >= 0) {
@@ -325,11 +328,13 @@ mdh_status pass_of(const ScanCall& c, const Plan& z, const Segments& segs, hipSt
 
 template <typename T, int V, int L>
 mdh_status step(const ScanCall& c, hipStream_t st) {
-  const int64_t blocks = cdiv((int64_t)c.D * L, 256);
-  const int64_t grid = blocks * c.B;
-  if (grid >= 1 << 24) return MDH_ERR_SIZE;
+  if (c.B * c.D >= (int64_t)1 << 25) return MDH_ERR_SIZE;  // (64 lanes a channel at the most: 2^31)
   clear_stale_error();
-  scan_step_kernel<T, V, L><<<(unsigned)grid, 256, 0, st>>>(c, (unsigned)blocks);
+  const int64_t lanes = (int64_t)c.D * L, blocks = cdiv(lanes, 256);
+  if (lanes >= 2048)  // (an eighth of the lanes without a channel at the most)
+    scan_step_kernel<T, V, L, true><<<(unsigned)(c.B * blocks), 256, 0, st>>>(c, (unsigned)blocks);
+  else
+    scan_step_kernel<T, V, L, false><<<(unsigned)cdiv(c.B * lanes, 256), 256, 0, st>>>(c, 0);
   return launch_status();
 }
 template <typename T>

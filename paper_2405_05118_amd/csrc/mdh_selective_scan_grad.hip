@@ -140,7 +140,9 @@ __global__ __launch_bounds__(64 * WAVES, NS == 1 && sizeof(T) == 2 ? 4 : 2) void
   // of the 512 sums of a tile (d_b and d_c of 16 tokens and 16 states) a thread adds up its own over the wavefronts
   static_assert(THREADS == 512, "a thread's sum of d_b or d_c");
   const int shared_t = (int)threadIdx.x / 16 % 4 * 4 + (int)threadIdx.x / 64 % 4, shared_n = p.j, per_token = c.G * c.N;
-  const int shared_at = shared_t * per_token + shared_n, which = __builtin_amdgcn_readfirstlane((int)threadIdx.x / 256);
+  // (B T G N < 2^32: of a token that there is less than that)
+  const unsigned shared_at = (unsigned)shared_t * (unsigned)per_token + (unsigned)shared_n;
+  const int which = __builtin_amdgcn_readfirstlane((int)threadIdx.x / 256);
   float* const shared_to = w.shared + ((which * (int64_t)blocks + p.block) * c.B + p.b) * c.T * per_token + (int64_t)p.g * c.N;
   int turn = 0;
   bool behind = false;  // a block's gradients lie in LDS

@@ -320,6 +320,13 @@ def _back(sizes, x=64, d_y=64, d_x=64, w=64, ws=1 << 20, nws=1 << 50, strides=No
                                               d_x, d_before, None, None, ws, nws, None)
 
 
+def test_refuses_outputs_whose_rows_overlap():
+    ok = (2, 5, 16, 4)
+    for strides in ([80, 16, 80, 15], [80, 16, 15, 16], [80, 16, 80, -15]):
+        assert _raw(ok, strides=strides) == E_SIZE
+    assert _back(ok, strides=[80, 16, 80, 16, 80, 15]) == E_SIZE and _back(ok, strides=[80, 16, 80, 16, 15, 16]) == E_SIZE
+
+
 def test_refusals():
     ok = (2, 5, 16, 4)
     for sizes in ((-1, 5, 16, 4), (2, -1, 16, 4), (2, 5, 0, 4), (2, 5, 16, 0), (1 << 16, 1 << 16, 16, 4), (2, 5, 1 << 24, 4), (1, (1 << 31) - 1, 8, 4)):
