@@ -680,7 +680,8 @@ mdh_status mdh_selective_scan(const int64_t* sizes, mdh_dtype dtype, const void*
  *            NULL: all dense.  Gradients of the activations overlap no input and are wanted all, d_gate where there is a gate.
  *   d_A, d_skip, d_dt_bias, d_initial_state  fp32, NULL: not wanted
  *   workspace  mdh_selective_scan_workspace_size(sizes, dtype, 1) bytes, which hold what the forward call wants too
- * Sums over channels (d_b, d_c) and over tokens (d_A, d_skip, d_dt_bias) are fp32, in a fixed order.
+ * B * T * G * N < 2^31 (MDH_ERR_SIZE).  Sums over channels (d_b, d_c) and over tokens (d_A, d_skip, d_dt_bias) are fp32, in a fixed
+ * order.
  */
 mdh_status mdh_selective_scan_backward(const int64_t* sizes, mdh_dtype dtype, const void* x, const void* dt, const void* gate,
                                        const void* b, const void* c, const void* d_y, const int64_t* strides, const float* A,

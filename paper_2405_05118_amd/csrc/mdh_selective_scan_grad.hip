@@ -140,7 +140,7 @@ __global__ __launch_bounds__(64 * WAVES, NS == 1 && sizeof(T) == 2 ? 4 : 2) void
   // of the 512 sums of a tile (d_b and d_c of 16 tokens and 16 states) a thread adds up its own over the wavefronts
   static_assert(THREADS == 512, "a thread's sum of d_b or d_c");
   const int shared_t = (int)threadIdx.x / 16 % 4 * 4 + (int)threadIdx.x / 64 % 4, shared_n = p.j, per_token = c.G * c.N;
-  // (B T G N < 2^32: of a token that there is less than that)
+  // (B T G N < 2^31: of a token that there is, less than that)
   const unsigned shared_at = (unsigned)shared_t * (unsigned)per_token + (unsigned)shared_n;
   const int which = __builtin_amdgcn_readfirstlane((int)threadIdx.x / 256);
   float* const shared_to = w.shared + ((which * (int64_t)blocks + p.block) * c.B + p.b) * c.T * per_token + (int64_t)p.g * c.N;
@@ -322,7 +322,7 @@ template <typename T, int NS, int WAVES>
 mdh_status pass(const ScanCall& c, const Shape& z, const Parts& w, hipStream_t st) {
   const int seg_blocks = (int)cdiv(c.E, kRows);
   const int64_t grid = c.B * z.n * c.G * z.blocks, seg_grid = c.B * z.n * c.G * seg_blocks, outs = cdiv(c.B * c.T * c.G * c.N, 256);
-  if (grid * z.waves >= 1 << 26 || (z.n > 1 && seg_grid >= 1 << 24) || outs >= 1 << 23) return MDH_ERR_SIZE;
+  if (grid * z.waves >= 1 << 26 || (z.n > 1 && seg_grid >= 1 << 24) || outs >= 1 << 23) return MDH_ERR_SIZE;  // 2^32 lanes
   clear_stale_error();
   if (z.n > 1) {
     grad_segments_kernel<T, NS><<<(unsigned)seg_grid, kThreads, 0, st>>>(c, w, seg_blocks);

@@ -352,36 +352,6 @@ def test_activations_past_2_31_elements():
 
 
 @gpu
-def test_sums_over_channels_past_2_31_elements():
-    """d_b and d_c of 17 tokens of 3.9 million groups of one channel: the bits that the same groups have in a call of their own."""
-    T, G, N = 17, 3900000, 64
-    assert 15 * G * N > 1 << 31 and T * G * N < 1 << 32
-    gen = torch.Generator(device="cuda").manual_seed(3)
-
-    def new(*shape, dtype=BF16):
-        return torch.empty(*shape, dtype=dtype, device="cuda").normal_(generator=gen)
-
-    some = torch.tensor([0, 1, G // 2, G - 2, G - 1], device="cuda")
-
-    def run(x, dt, d_y, A, b, c):
-        D = x.shape[-1]
-        sizes = (1, T, D, N, D)
-        kept = torch.empty(mdh.mdh_selective_scan_checkpoints_size(sizes), dtype=torch.uint8, device="cuda")
-        ws = torch.empty(max(mdh.mdh_selective_scan_workspace_size(sizes, BF16, True), 4), dtype=torch.uint8, device="cuda")
-        mdh.mdh_selective_scan(x, dt, A, b, c, torch.empty_like(x), checkpoints=kept, softplus=True, workspace=ws)
-        d_b, d_c = torch.full_like(b, NAN), torch.full_like(c, NAN)
-        mdh.mdh_selective_scan_backward(x, dt, A, b, c, d_y, torch.empty_like(x), torch.empty_like(dt), None, d_b, d_c, kept, softplus=True,
-                                        workspace=ws)
-        return d_b, d_c
-
-    x, dt, d_y = (new(1, T, G) for _ in range(3))
-    A, b, c = -new(G, N, dtype=F32).abs(), new(1, T, G, N), new(1, T, G, N)
-    for all_of, few in zip(run(x, dt, d_y, A, b, c), run(*(v[..., some].contiguous() for v in (x, dt, d_y)), A[some], b[:, :, some].contiguous(),
-                                                         c[:, :, some].contiguous())):
-        assert few.isfinite().all() and few.float().abs().sum() > 0 and torch.equal(all_of[:, :, some], few)
-
-
-@gpu
 def test_prompt_then_tokens():
     """A prompt and the tokens after it, one at a time, are one sequence."""
     p = Problem(F32, 2, 60, 40, 16, 2)
@@ -554,6 +524,10 @@ def test_refusals():
                                                                            state, None, 0, 64, None)
     assert step((2, 8, 16, 3)) == E_SIZE and step((2, 8, 65, 1)) == E_UNSUP and step((1 << 22, 8, 16, 1)) == E_SIZE
     assert step((2, 8, 16, 1), x=None) == E_NULL and step((2, 8, 16, 1), state=None) == E_NULL and step((0, 8, 16, 1)) == 0
+
+
+def test_refuses_gradients_of_b_and_c_past_2_31_elements():
+    assert _back((1, 17, 3900000, 64, 3900000)) == E_SIZE and _back((1, 1 << 21, 64, 64, 16)) == E_SIZE
 
 
 def test_refuses_outputs_whose_rows_overlap():
