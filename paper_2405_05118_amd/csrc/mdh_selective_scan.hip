@@ -44,11 +44,12 @@ __global__ __launch_bounds__(F::THREADS) void scan_kernel(ScanCall c, Segments s
   constexpr int S = NS * 16, CH = F::CH, W = F::W, TOKENS = F::TOKENS, NA = STATES_ONLY ? 2 : 3, NB = STATES_ONLY ? 1 : 2;
   typedef Stage<T, NA, NB, CH, S, TOKENS, F::THREADS> In;
   typedef Outputs<T, 1, CH, TOKENS, F::THREADS> Out;
-  __shared__ T raw[NA * TOKENS * CH] __attribute__((aligned(16)));
-  __shared__ float bc[NB * In::kFloats] __attribute__((aligned(16)));
+  // two buffers where they do not cost a workgroup its place: the next block is staged while one is worked on, one barrier less
+  constexpr int BUFFERS = W > 1 && NS == 1 ? 2 : 1, RAW = NA * TOKENS * CH, BC = NB * In::kFloats;
+  __shared__ T raws[BUFFERS * RAW] __attribute__((aligned(16)));
+  __shared__ float bcs[BUFFERS * BC] __attribute__((aligned(16)));
   __shared__ float sums[STATES_ONLY ? 1 : F::THREADS / 64][STATES_ONLY ? 4 : kSumFloats] __attribute__((aligned(16)));
   __shared__ float2 ends[W > 1 ? W : 1][W > 1 ? CH * S : 1];
-  T *const xs = raw, *const dts = raw + TOKENS * CH, *const gates = raw + 2 * TOKENS * CH;
   ScanPlace p = scan_place(c, blocks, segs.n, segs.tokens);
   const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6, tile = W > 1 ? __builtin_amdgcn_readfirstlane(p.row / CH) : 0;
   p.row %= CH;
@@ -87,13 +88,17 @@ __global__ __launch_bounds__(F::THREADS) void scan_kernel(ScanCall c, Segments s
   };
   Out out;
   if (!STATES_ONLY) out.begin(c.out, p, p.first, 1, d0, width);
-  for (int64_t t0 = p.first; t0 < p.alive; t0 += TOKENS) {
-    if (!STATES_ONLY && t0 > p.first) out.take(raw);
-    in.stage(raw, bc);
+  if (p.first < p.alive) {
+    in.stage(raws, bcs);
     __syncthreads();
-    // (stores go out behind the wait for the block's loads: what is waited for next has been under way for long)
-    if (!STATES_ONLY && t0 > p.first) out.store(TOKENS);
-    if (t0 + TOKENS < p.alive) in.load(p.alive - t0 - TOKENS);
+    if (p.first + TOKENS < p.alive) in.load(p.alive - p.first - TOKENS);
+  }
+  int turn = 0;
+  for (int64_t t0 = p.first; t0 < p.alive; t0 += TOKENS) {
+    T* const raw = raws + turn * RAW;
+    const float* const bc = bcs + turn * BC;
+    T *const xs = raw, *const dts = raw + TOKENS * CH, *const gates = raw + 2 * TOKENS * CH;
+    const bool more = t0 + TOKENS < p.alive;
     const int tokens = (int)min((int64_t)TOKENS, p.alive - t0);
     for (int i0 = tile * kTile; i0 < (W > 1 ? (tile + 1) * kTile : tokens); i0 += kTile) {
       const int at = place_of<T, CH>(i0 + p.j, p.row);
@@ -173,13 +178,19 @@ __global__ __launch_bounds__(F::THREADS) void scan_kernel(ScanCall c, Segments s
         xs[at] = from_float<T>(live ? v : 0.f);  // where x was
       }
     }
+    if (BUFFERS == 2) turn ^= 1;
+    if (BUFFERS == 2 && more) in.stage(raws + turn * RAW, bcs + turn * BC);
     __syncthreads();
+    if (!STATES_ONLY) out.take(raw);  // (a lane's own pieces, before it stages others in their place)
+    if (BUFFERS == 1 && more) {
+      in.stage(raws, bcs);
+      __syncthreads();
+    }
+    // (stores go out behind the wait for the block's loads: what is waited for next has been under way for long)
+    if (!STATES_ONLY) out.store(p.last - t0);
+    if (t0 + 2 * TOKENS < p.alive) in.load(p.alive - t0 - 2 * TOKENS);
   }
   if (!STATES_ONLY) {
-    if (p.first < p.alive) {
-      out.take(raw);
-      out.store(p.last - p.first - (p.alive - p.first - 1) / TOKENS * TOKENS);
-    }
     store_zeros<T, CH, F::THREADS>(c.out[0], p, d0, width, TOKENS);
   }
   if (!mine || tile) return;
