@@ -31,6 +31,9 @@ EXPORTS = (
     "mdh_static_scratch_bytes", "mdh_scan_timed_out",
     "mdh_linattn_workspace_size", "mdh_linattn", "mdh_linattn_backward", "mdh_linattn_step",
     "mdh_group_norm_workspace_size", "mdh_group_norm", "mdh_group_norm_backward",
+    "mdh_causal_conv_workspace_size", "mdh_causal_conv", "mdh_causal_conv_backward", "mdh_causal_conv_step",
+    "mdh_selective_scan_workspace_size", "mdh_selective_scan_checkpoints_size", "mdh_selective_scan", "mdh_selective_scan_backward",
+    "mdh_selective_scan_step", "mdh_layer_norm_workspace_size", "mdh_layer_norm", "mdh_layer_norm_backward",
 )
 MDH_F32, MDH_BF16 = 0, 1
 MDH_ACT_NONE, MDH_ACT_RELU, MDH_ACT_SILU, MDH_ACT_GELU = range(4)
