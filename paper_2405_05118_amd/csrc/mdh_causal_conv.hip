@@ -16,7 +16,7 @@ namespace mdh {
 namespace {
 
 constexpr int kThreads = 256;
-constexpr int kAhead = 4, kBackAhead = 8;  // rows whose loads are under way together
+constexpr int kAhead = 4;  // rows whose loads are under way together
 
 // lanes along the channels (2^k of them), the other lanes of a workgroup are runs; then blocks of channels, runs, sequences
 struct Grid {
@@ -58,14 +58,14 @@ __device__ __forceinline__ RowWords<T, V> line(const ConvCall& c, const Place& p
   if (t < 0 && c.s_in && p.slot >= 0) return load_row<T, V>(window_at<T>(c, c.s_in, p.slot, c.W - 1 + t, p.ch), p.left);
   return 0;
 }
-// N rows from p on, those before `end`
+// N rows from p on, those before `end`; as they are wanted, part_of() each
 template <typename T, int V, int N>
 __device__ __forceinline__ void rows_of(const TokenView& v, const Place& p, int64_t t, int64_t end, RowWords<T, V> (&w)[N]) {
   const T* from = at<T>(v, p.b, t, p.ch);
 #pragma unroll
   for (int u = 0; u < N; ++u) {
     w[u] = 0;
-    if (t + u < end) w[u] = load_row<T, V>(from + u * v.st, p.left);
+    if (t + u < end) w[u] = load_part<T, V>(from + u * v.st, p.left, p.ch >= V);
   }
 }
 template <typename T, int W, int V>
@@ -125,7 +125,7 @@ __global__ __launch_bounds__(kThreads) void conv_kernel(ConvCall c, Grid g) {
     for (int u = 0; u < kAhead; ++u) {
       if (t + u >= t1) break;
       float x[V], z[V], y[V];
-      unpack_row<T, V>(raw[u], x);
+      unpack_row<T, V>(part_of<T, V>(raw[u], p.left, p.ch >= V), x);
       shift<W, V>(window, x);
       taps<W, V>(w, bias, window, z);
       act_of<V>(c.act, z, y);
@@ -138,6 +138,7 @@ __global__ __launch_bounds__(kThreads) void conv_kernel(ConvCall c, Grid g) {
 // open[j]: gradient of X_{t-W+1+j} as far as the tokens up to t give it
 template <typename T, int W, int V>
 __global__ __launch_bounds__(kThreads) void conv_backward_kernel(ConvCall c, Grid g) {
+  constexpr int AHEAD = sizeof(T) == 2 ? 8 : 4;  // (fp32 rows are twice the registers: one wavefront a SIMD with eight)
   const Place p = place<V>(c, g);
   // rows of the gradient: this run's, the window's before the first run's
   const int64_t t1 = min(p.t0 + g.run, c.T), first = p.t0 ? p.t0 : -(int64_t)(W - 1), end = t1 + W - 1;
@@ -149,7 +150,7 @@ __global__ __launch_bounds__(kThreads) void conv_backward_kernel(ConvCall c, Gri
     for (int j = 0; j < W; ++j) dw[j][i] = 0.f;
   }
   if (p.left > 0 && (p.t0 < c.T || p.t0 == 0)) {
-    RowWords<T, V> next_x[kBackAhead], next_dy[kBackAhead];
+    RowWords<T, V> next_x[AHEAD], next_dy[AHEAD];
     const int64_t readable = min(end, p.len);
     rows_of<T, V>(c.x, p, p.t0, readable, next_x);
     rows_of<T, V>(c.y, p, p.t0, readable, next_dy);
@@ -161,20 +162,20 @@ __global__ __launch_bounds__(kThreads) void conv_backward_kernel(ConvCall c, Gri
       for (int i = 0; i < V; ++i) open[j][i] = 0.f;
     }
     filter<T, W, V>(c, p, w, bias);
-    for (int64_t t = p.t0; t < end; t += kBackAhead) {
-      RowWords<T, V> rx[kBackAhead], ry[kBackAhead];
+    for (int64_t t = p.t0; t < end; t += AHEAD) {
+      RowWords<T, V> rx[AHEAD], ry[AHEAD];
 #pragma unroll
-      for (int u = 0; u < kBackAhead; ++u) rx[u] = next_x[u], ry[u] = next_dy[u];
-      if (t + kBackAhead < end) {
-        rows_of<T, V>(c.x, p, t + kBackAhead, readable, next_x);
-        rows_of<T, V>(c.y, p, t + kBackAhead, readable, next_dy);
+      for (int u = 0; u < AHEAD; ++u) rx[u] = next_x[u], ry[u] = next_dy[u];
+      if (t + AHEAD < end) {
+        rows_of<T, V>(c.x, p, t + AHEAD, readable, next_x);
+        rows_of<T, V>(c.y, p, t + AHEAD, readable, next_dy);
       }
 #pragma unroll
-      for (int u = 0; u < kBackAhead; ++u) {
+      for (int u = 0; u < AHEAD; ++u) {
         if (t + u >= end) break;
         float x[V], dy[V], z[V], y[V], slope[V];
-        unpack_row<T, V>(rx[u], x);
-        unpack_row<T, V>(ry[u], dy);
+        unpack_row<T, V>(part_of<T, V>(rx[u], p.left, p.ch >= V), x);
+        unpack_row<T, V>(part_of<T, V>(ry[u], p.left, p.ch >= V), dy);
         shift<W, V>(window, x);
         taps<W, V>(w, bias, window, z);
         act_slope<V>(c.act, z, y, slope);
@@ -280,10 +281,21 @@ Grid grid_of(const ConvCall& c, Which which) {
   g.k = 0;
   while (g.k < (which == kStep ? 8 : which == kBackward ? 5 : 6) && 1 << g.k < lanes) ++g.k;
   g.blocks = cdiv(lanes, 1 << g.k);
-  // runs of 64 tokens, shorter ones while there are fewer than three (backward two) wavefronts a SIMD
+  const auto groups = [&](int64_t run) { return c.T ? cdiv(c.T, run * (kThreads >> g.k)) : 1; };
+  // runs of 64 tokens, shorter ones while there are fewer than three wavefronts a SIMD
   g.run = which == kStep ? 1 : 64;
-  while (g.run > 8 && lanes * c.B * cdiv(c.T, g.run) < 1024 * 64 * (which == kForward ? 3 : 2)) g.run /= 2;
-  g.groups = c.T ? cdiv(c.T, (int64_t)g.run * (kThreads >> g.k)) : 1;
+  while (which == kForward && g.run > 8 && lanes * c.B * cdiv(c.T, g.run) < 1024 * 64 * 3) g.run /= 2;
+  // Backward two workgroups a compute unit are at work, and some left over take as long as all of them (4 x 2048 x 4104 in runs of 64:
+  // 528 workgroups, 130 us; 4096 channels are 512, 62): the run with the least rounds of them times its rows, 12 of them
+  // for the start and the rows of the run before.
+  if (which == kBackward) {
+    int64_t least = 0;
+    for (int run = 8; run <= 128; run += 8) {
+      const int64_t time = cdiv(g.blocks * groups(run) * c.B, 512) * (run + 12);
+      if (run == 8 || time <= least) g.run = run, least = time;
+    }
+  }
+  g.groups = groups(g.run);
   return g;
 }
 

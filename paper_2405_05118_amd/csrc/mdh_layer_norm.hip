@@ -197,9 +197,9 @@ __global__ __launch_bounds__(L > 256 ? L : 256) void layer_norm_backward_kernel(
       const int ch = (k * L + l) * V, left = live ? c.C - ch : 0;
       r.x[k] = r.y[k] = r.t[k] = (Word4){0, 0, 0, 0};
       if (left <= 0) continue;
-      r.x[k] = load_row<T>(at<T>(c.x, row, ch), left);
-      r.y[k] = load_row<T>(at<T>(c.y, row, ch), left);
-      if (c.dtotal.p) r.t[k] = load_row<T>(at<T>(c.dtotal, row, ch), left);
+      r.x[k] = load_part<T>(at<T>(c.x, row, ch), left, ch >= V);
+      r.y[k] = load_part<T>(at<T>(c.y, row, ch), left, ch >= V);
+      if (c.dtotal.p) r.t[k] = load_part<T>(at<T>(c.dtotal, row, ch), left, ch >= V);
     }
   };
   constexpr bool AHEAD = L < 1024;  // (1024 lanes have 128 registers each)
@@ -210,7 +210,13 @@ __global__ __launch_bounds__(L > 256 ? L : 256) void layer_norm_backward_kernel(
   for (; first < c.rows; first += step) {
     const int64_t row = first + threadIdx.x / L;
     if (!AHEAD) load(next, row);
-    const Row r = next;
+    Row r = next;
+    if (row < c.rows)
+#pragma unroll
+      for (int k = 0; k < P; ++k) {
+        const int ch = (k * L + l) * V, left = c.C - ch;
+        r.x[k] = part_of<T>(r.x[k], left, ch >= V), r.y[k] = part_of<T>(r.y[k], left, ch >= V), r.t[k] = part_of<T>(r.t[k], left, ch >= V);
+      }
     if (AHEAD && first + step < c.rows) load(next, row + step);
     float s1 = 0.f, s2 = 0.f;
 #pragma unroll

@@ -36,6 +36,31 @@ __device__ __forceinline__ RowWords<T, V> load_row(const T* p, int left) {
     }
   return w;
 }
+// The same for loads that other work goes on beside: the last values of a row come as the V that end there, in one access (value by value a
+// wavefront waits for each before it goes on), and part_of() moves them to their places when they are wanted
+// (a row's last lane, backward: norm of 8192 x 4097 111 us, so 79; convolution of 4 x 2048 x 4097 fp32 160, so 99).
+// inside: V values or more lie in the row before p.
+template <typename T, int V = kLaneValues<T>>
+__device__ __forceinline__ RowWords<T, V> load_part(const T* p, int left, bool inside) {
+  if (left < V && !inside) return load_row<T, V>(p, left);
+  return *(const typename WordsOf<V * (int)sizeof(T) / 4>::any*)(p - (left < V ? V - left : 0));
+}
+template <typename T, int V = kLaneValues<T>>
+__device__ __forceinline__ RowWords<T, V> part_of(RowWords<T, V> w, int left, bool inside) {
+  if (left <= 0 || left >= V || !inside) return w;
+  const int bits = (V - left) * (int)sizeof(T) * 8;
+  uint64_t low = (uint64_t)w[1] << 32 | w[0];
+  if constexpr (V * sizeof(T) == 8) {
+    low >>= bits;
+  } else {
+    const uint64_t high = (uint64_t)w[3] << 32 | w[2];
+    low = bits < 64 ? low >> bits | high << (64 - bits) : high >> (bits - 64);
+    const uint64_t rest = bits < 64 ? high >> bits : 0;
+    w[2] = (uint32_t)rest, w[3] = (uint32_t)(rest >> 32);
+  }
+  w[0] = (uint32_t)low, w[1] = (uint32_t)(low >> 32);
+  return w;
+}
 template <typename T, int V = kLaneValues<T>>
 __device__ __forceinline__ void store_row(T* p, int left, const RowWords<T, V>& w) {
   if (left >= V) {
