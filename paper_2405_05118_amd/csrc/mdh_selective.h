@@ -44,14 +44,16 @@ __device__ __forceinline__ float again(float v) {
 // 2^x by the hardware (1 ulp; 0 below 2^-126)
 __device__ __forceinline__ float exp2_of(float x) { return __builtin_amdgcn_exp2f(x); }
 
-// The factor 2^(delta A) of a state.  v_exp_f32 is too small by 0.12 2^-24 on average where its result is just below 1 (a million
-// arguments from -1e-2 to -1e-5; no more than 0.7 2^-24 at any), which a state that decays slowly adds up over its thousands of tokens:
-// 1e-8 more in the exponent (2^0 stays 1) takes final states and gradients of 1001 tokens from 1.9e-6 to 8e-7 off.  One more instruction
-// where delta is broadcast; left out for bf16, whose operands are off by 2^-9.
-template <typename T>
-__device__ __forceinline__ float factor_of(float delta, float A) {
-  return exp2_of(sizeof(T) == 4 ? fmaf(delta, A, 1e-8f) : delta * A);
+// v_exp_f32 is too small by 0.12 2^-24 on average where its result is just below 1 (a million arguments from -1e-2 to -1e-5; no more than
+// 0.7 2^-24 at any), which a state that decays slowly adds up over its thousands of tokens.  The tokens of a tile that had a factor
+// other than 1, in lane j token j's delta, times that: what a state grows by once a tile (7e-9 h; with no such token it stays as it is, an
+// infinite one too).  The final state and d_A of 1001 tokens: 1.9e-6 off without.
+__device__ __forceinline__ float growth(float delta, int lane) {
+  const unsigned moved = (unsigned)(__ballot(delta != 0.f) >> (lane & 48)) & 0xffffu;
+  return fmaf((float)__builtin_popcount(moved), 7e-9f, 1e-30f);
 }
+// the same in the exponent, for a token alone (2^0 stays 1)
+__device__ __forceinline__ float factor_of(float delta, float A) { return exp2_of(fmaf(delta, A, 1e-8f)); }
 
 // e^v with the rounding of v log2(e) put right
 __device__ __forceinline__ float exp_of(float v) {

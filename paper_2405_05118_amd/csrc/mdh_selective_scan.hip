@@ -104,7 +104,7 @@ __global__ __launch_bounds__(F::THREADS) void scan_kernel(ScanCall c, Segments s
       const int at = place_of<T, CH>(i0 + p.j, p.row);
       const bool live = i0 + p.j < tokens;
       const Token k = token_of(c, to_float(xs[at]), to_float(dts[at]), live, dt_bias);
-      const float u = k.delta * k.x;
+      const float u = k.delta * k.x, grow = growth(k.delta, lane);
       total += k.delta;
       float y[kTile];
       const float* bs = bc + p.j * In::kPitch + i0;
@@ -117,11 +117,13 @@ __global__ __launch_bounds__(F::THREADS) void scan_kernel(ScanCall c, Segments s
             const Float4 bt = four_of(bs + s * 16 * In::kPitch + Q), ct = four_of(bs + (STATES_ONLY ? 0 : In::kFloats) + s * 16 * In::kPitch + Q);
             unroll<4>([&](auto i) {
               constexpr int I = decltype(i)::value;
-              const float a = factor_of<T>(lane_of_row<Q + I>(k.delta), A[s]);
+              const float a = exp2_of(lane_of_row<Q + I>(k.delta) * A[s]);
               h[s] = fmaf(a, h[s], lane_of_row<Q + I>(u) * bt[I]);
               if (!STATES_ONLY) y[Q + I] = s ? fmaf(ct[I], h[s], y[Q + I]) : ct[I] * h[s];
             });
           });
+#pragma unroll
+        for (int s = 0; s < NS; ++s) h[s] = fmaf(h[s], grow, h[s]);
       } else {
         float own[NS][kTile], product[NS][kTile];
 #pragma unroll
@@ -132,13 +134,13 @@ __global__ __launch_bounds__(F::THREADS) void scan_kernel(ScanCall c, Segments s
             const Float4 bt = four_of(bs + s * 16 * In::kPitch + Q);
             unroll<4>([&](auto i) {
               constexpr int I = decltype(i)::value;
-              const float a = factor_of<T>(lane_of_row<Q + I>(k.delta), A[s]);
+              const float a = exp2_of(lane_of_row<Q + I>(k.delta) * A[s]);
               from_zero = fmaf(a, from_zero, lane_of_row<Q + I>(u) * bt[I]);
               all *= a;
               own[s][Q + I] = from_zero, product[s][Q + I] = all;
             });
           });
-          ends[tile][(s * CH + p.row) * 16 + p.j] = make_float2(from_zero, all);
+          ends[tile][(s * CH + p.row) * 16 + p.j] = make_float2(from_zero, fmaf(all, grow, all));
         }
         __syncthreads();
         float before[NS];
@@ -257,7 +259,7 @@ __global__ __launch_bounds__(256) void scan_step_kernel(ScanCall c, unsigned blo
       const Token k = token_of(c, x, dt, true, c.dt_bias ? c.dt_bias[d] : 0.f);
 #pragma unroll
       for (int s = 0; s < V; ++s) {
-        h[s] = fmaf(factor_of<float>(k.delta, A[s]), h[s], k.delta * k.x * bt[s]);
+        h[s] = fmaf(factor_of(k.delta, A[s]), h[s], k.delta * k.x * bt[s]);
         y = fmaf(ct[s], h[s], y);
       }
       *(fv*)state = h;

@@ -68,16 +68,19 @@ __global__ __launch_bounds__(kThreads) void grad_segments_kernel(ScanCall c, Par
       float dp = to_float(dys[at]);
       if (c.in[2].p) dp *= gate_of(to_float(gates[at]));
       total += k.delta;
+      const float grow = growth(k.delta, threadIdx.x & 63);
 #pragma unroll
-      for (int s = 0; s < NS; ++s)
+      for (int s = 0; s < NS; ++s) {
         unroll<kTile / 4>([&](auto quarter) {
           constexpr int Q = kTile - 4 - decltype(quarter)::value * 4;
           const Float4 ct = four_of(cs + (s * 16 + p.j) * In::kPitch + i0 + Q);
           unroll<4>([&](auto i) {
             constexpr int I = 3 - decltype(i)::value;
-            e[s] = factor_of<T>(lane_of_row<Q + I>(k.delta), A[s]) * fmaf(lane_of_row<Q + I>(dp), ct[I], e[s]);
+            e[s] = exp2_of(lane_of_row<Q + I>(k.delta) * A[s]) * fmaf(lane_of_row<Q + I>(dp), ct[I], e[s]);
           });
         });
+        e[s] = fmaf(e[s], grow, e[s]);
+      }
     }
     __syncthreads();
   }
@@ -170,6 +173,7 @@ __global__ __launch_bounds__(64 * WAVES, NS == 1 && sizeof(T) == 2 ? 4 : 2) void
       const int at = place_of<T, CH>(i0 + p.j, p.row);
       const Token k = token_of(c, to_float(xs[at]), to_float(dts[at]), live, dt_bias);
       const float dy = to_float(dys[at]), dp = c.in[2].p ? dy * gate_of(to_float(gates[at])) : dy, u = k.delta * k.x;
+      const float grow = growth(k.delta, lane);
       float sp = 0.f, sr = 0.f, sq = 0.f;
       float* own = sums[wave];
 #pragma unroll
@@ -182,7 +186,7 @@ __global__ __launch_bounds__(64 * WAVES, NS == 1 && sizeof(T) == 2 ? 4 : 2) void
           const Float4 bt = four_of(bs + Q), ct = four_of(bs + In::kFloats + Q);
           unroll<4>([&](auto i) {
             constexpr int I = Q + decltype(i)::value;
-            a[I] = factor_of<T>(lane_of_row<I>(k.delta), A[s]);
+            a[I] = exp2_of(lane_of_row<I>(k.delta) * A[s]);
             h[I + 1] = fmaf(a[I], h[I], lane_of_row<I>(u) * bt[I - Q]);
             own[I * kSumPitch + lane] = ct[I - Q] * h[I + 1];
           });
@@ -217,6 +221,7 @@ __global__ __launch_bounds__(64 * WAVES, NS == 1 && sizeof(T) == 2 ? 4 : 2) void
             add_lane_of_row<I>(dA[s], delta2, a[I]);
           });
         });
+        e[s] = fmaf(e[s], grow, e[s]);
         wave_fence();
         sr += row_sum(own, lane);
         settle(sr), settle(dA[s]), settle(e[s]);

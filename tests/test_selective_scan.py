@@ -175,20 +175,23 @@ def test_long_sequences(dtype, B, T, D, N, G):
 
 
 @gpu
+@pytest.mark.parametrize("dtype", [F32, BF16])
 @pytest.mark.parametrize("B,T,D,N", [(1, 16384, 16, 16), (1, 16000, 4096, 16), (4, 8192, 4096, 8), (1, 9000, 4, 40)])
-def test_slow_decays_add_up_no_bias(B, T, D, N):
+def test_slow_decays_add_up_no_bias(dtype, B, T, D, N):
     """Time steps of about 2^-13 that differ from token to token (with one for all of them a factor's rounding would be the same each time,
     up to T u / 2 in all): h_T = sum of delta_t a^(T-t), the gradient of what it began with a^T, the same for every channel.
     Factors and states are each rounded with half a step or so of random sign: 0.5 u of a token, sqrt(T / N) of that in the mean over N
     states, four times which are allowed.  What is of one sign adds up: less than a sixteenth of a step, T u / 16.  32 u for the rest."""
     delta = torch.rand(T, generator=torch.Generator().manual_seed(1)) * 2.0 ** -13 + 2.0 ** -14
-    A = (-1 - torch.arange(N) / 16.0).expand(D, N).contiguous().cuda()
-    x, dt = torch.ones(B, T, D, device="cuda"), delta.cuda()[None, :, None].expand(B, T, D).contiguous()
-    b, c = torch.ones(B, T, 1, N, device="cuda"), torch.zeros(B, T, 1, N, device="cuda")
+    delta = delta.to(dtype).float()
+    # (sixteenths of a bf16 step are on the grid of the factors: correctly rounded ones, too, would all be off to one side, by 1000 u)
+    A = (-1 - (torch.arange(N) / 16.0 if dtype == F32 else torch.rand(N, generator=torch.Generator().manual_seed(2)))).expand(D, N).contiguous().cuda()
+    x, dt = torch.ones(B, T, D, dtype=dtype, device="cuda"), delta.to(dtype).cuda()[None, :, None].expand(B, T, D).contiguous()
+    b, c = torch.ones(B, T, 1, N, dtype=dtype, device="cuda"), torch.zeros(B, T, 1, N, dtype=dtype, device="cuda")
     y, end, begin = torch.empty_like(x), torch.empty(B, D, N, device="cuda"), torch.empty(B, D, N, device="cuda")
     sizes = (B, T, D, N, 1)
     kept = torch.empty(mdh.mdh_selective_scan_checkpoints_size(sizes), dtype=torch.uint8, device="cuda")
-    ws = torch.empty(mdh.mdh_selective_scan_workspace_size(sizes, F32, True), dtype=torch.uint8, device="cuda")
+    ws = torch.empty(mdh.mdh_selective_scan_workspace_size(sizes, dtype, True), dtype=torch.uint8, device="cuda")
     mdh.mdh_selective_scan(x, dt, A, b, c, y, final_state=end, checkpoints=kept, workspace=ws)
     d_x, d_dt, d_b, d_c = (torch.empty_like(v) for v in (x, dt, b, c))
     mdh.mdh_selective_scan_backward(x, dt, A, b, c, 0 * x, d_x, d_dt, torch.empty_like(A), d_b, d_c, kept, d_final_state=torch.ones_like(end),
