@@ -772,9 +772,10 @@ def mdh_selective_scan_step(x, dt, A, b, c, state, y, skip=None, gate=None, dt_b
     a pool (n, D, N)."""
     L = _lib or lib()
     B, D = shape = x.shape
-    N, G = A.shape[1], b.shape[1]
+    channels, N = A.shape
+    _, G, _ = b.shape
     shared = (B, G, N)  # (a call is as fast as the host is: nothing is looked at twice)
-    if (A.shape[0] != D or dt.shape != shape or y.shape != shape or b.shape != shared or c.shape != shared
+    if (channels != D or dt.shape != shape or y.shape != shape or b.shape != shared or c.shape != shared
             or (gate is not None and gate.shape != shape)):
         _scan_operands((B,), x, A, b, c, dt, (y, "y"), (gate, "gate"))
     ty = x.dtype

@@ -559,3 +559,16 @@ def test_binding_refuses_what_does_not_fit():
         mdh.mdh_selective_scan_step(x[:, 0], x[:, 0], A, b[:, 0], b[:, 0], torch.zeros(2, 8, 5), x[:, 0])
     with pytest.raises(TypeError):
         mdh.mdh_selective_scan_workspace_size((2, 5, 8, 4, 2), torch.float64)
+
+
+def test_binding_refuses_steps_that_do_not_fit():
+    x, A, b, h = torch.zeros(2, 8), torch.zeros(8, 4), torch.zeros(2, 2, 4), torch.zeros(2, 8, 4)
+    with pytest.raises(TypeError):
+        mdh.mdh_selective_scan_step(x, x, A, b, b, h, x)  # not on the GPU
+    for bad in ((x[:1], x, A, b, b, h, x), (x, x[:1], A, b, b, h, x), (x, x, A[:4], b, b, h, x), (x, x, A[..., None], b, b, h, x),
+                (x, x, A[0], b, b, h, x), (x, x, A, b[0], b, h, x), (x, x, A, b[..., :2], b, h, x), (x, x, A, b, b[:, :1], h, x),
+                (x, x, A, b, b, h, x[:, :4]), (x[None], x, A, b, b, h, x)):
+        with pytest.raises(ValueError):
+            mdh.mdh_selective_scan_step(*bad)
+    with pytest.raises(ValueError):
+        mdh.mdh_selective_scan_step(x, x, A, b, b, h, x, gate=x[:1])
