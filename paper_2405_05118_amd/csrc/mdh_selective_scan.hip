@@ -299,7 +299,7 @@ Plan plan(const ScanCall& c) {
   if (cut < best) z.W = 1;
   const int block = z.W == 8 ? 128 : ns == 4 ? 32 : 64;
   const int64_t in_all = cdiv(T, block);
-  int64_t n = cut < best ? cdiv(3072, groups) : 1;
+  int64_t n = cut < best ? cdiv(12 * 256, groups) : 1;  // (twelve workgroups a compute unit)
   if (n > in_all) n = in_all;
   if (n < 1) n = 1;
   const int64_t each = in_all ? cdiv(in_all, n) : 1;
