@@ -138,7 +138,7 @@ __global__ __launch_bounds__(kThreads) void conv_kernel(ConvCall c, Grid g) {
 // open[j]: gradient of X_{t-W+1+j} as far as the tokens up to t give it
 template <typename T, int W, int V>
 __global__ __launch_bounds__(kThreads) void conv_backward_kernel(ConvCall c, Grid g) {
-  constexpr int AHEAD = sizeof(T) == 2 ? 8 : 4;  // (fp32 rows are twice the registers: one wavefront a SIMD with eight)
+  constexpr int AHEAD = sizeof(T) == 2 ? 8 : 4;  // (rows ahead: four of bf16 65 us for 62; eight of fp32 leave one wavefront a SIMD)
   const Place p = place<V>(c, g);
   // rows of the gradient: this run's, the window's before the first run's
   const int64_t t1 = min(p.t0 + g.run, c.T), first = p.t0 ? p.t0 : -(int64_t)(W - 1), end = t1 + W - 1;
