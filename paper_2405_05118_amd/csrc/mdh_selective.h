@@ -44,16 +44,26 @@ __device__ __forceinline__ float again(float v) {
 // 2^x by the hardware (1 ulp; 0 below 2^-126)
 __device__ __forceinline__ float exp2_of(float x) { return __builtin_amdgcn_exp2f(x); }
 
-// v_exp_f32 is too small by 0.12 2^-24 on average where its result is just below 1 (a million arguments from -1e-2 to -1e-5; no more than
-// 0.7 2^-24 at any), which a state that decays slowly adds up over its thousands of tokens.  The tokens of a tile that had a factor
-// other than 1, in lane j token j's delta, times that: what a state grows by once a tile (7e-9 h; with no such token it stays as it is, an
-// infinite one too).  The final state and d_A of 1001 tokens: 1.9e-6 off without.
-__device__ __forceinline__ float growth(float delta, int lane) {
-  const unsigned moved = (unsigned)(__ballot(delta != 0.f) >> (lane & 48)) & 0xffffu;
-  return fmaf((float)__builtin_popcount(moved), 7e-9f, 1e-30f);
-}
-// the same in the exponent, for a token alone (2^0 stays 1)
+// A state that decays slowly multiplies thousands of factors just below 1, each of them rounded, and v_exp_f32 is besides too small by
+// 0.12 2^-24 on average there (a million arguments from -1e-2 to -1e-5; no more than 0.7 2^-24 at any).  So a state goes over a tile of
+// tokens by the factor of the tile, e^(A sum of deltas), one exponential for 16 tokens: what the tokens' own factors are off by does not
+// add up beyond their tile, and states that do not decay, or by less than 32 bits can tell a token, are held.
+// 1e-8 more in the exponent makes up for the mean (2^0 stays 1).
 __device__ __forceinline__ float factor_of(float delta, float A) { return exp2_of(fmaf(delta, A, 1e-8f)); }
+// the sum of the 16 lanes of a row, the same bits in all of them
+template <int N>
+__device__ __forceinline__ float add_rotated(float v) {
+  return v + __int_as_float(__builtin_amdgcn_mov_dpp(__float_as_int(v), 0x120 + N, 0xf, 0xf, true));
+}
+// a tile's sum of deltas, bounded: of steps near the largest number it would be infinite, and NaN times an A of 0
+__device__ __forceinline__ float sum_of_row(float delta) {
+  return add_rotated<1>(add_rotated<2>(add_rotated<4>(add_rotated<8>(__builtin_amdgcn_fmed3f(delta, -1e37f, 1e37f)))));
+}
+// What is to be added to a state behind a tile that began with `before` and was multiplied by `product` where `factor` is right.
+// (An infinite state is infinite behind the tile too; its difference of factors may be 0.)
+__device__ __forceinline__ float put_right(float factor, float product, float before) {
+  return (factor - product) * __builtin_amdgcn_fmed3f(before, -3e38f, 3e38f);
+}
 
 // e^v with the rounding of v log2(e) put right
 __device__ __forceinline__ float exp_of(float v) {

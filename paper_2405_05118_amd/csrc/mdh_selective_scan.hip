@@ -9,7 +9,8 @@
 // De-composition.  A row of 16 lanes is a channel, a lane one state of every 16; a wavefront has four channels, a workgroup 8 or 16.
 // Tokens are walked in tiles of 16.  Lane j loads x, dt and gate of token j, takes the softplus, and a step's delta reaches the row's
 // other lanes as a modifier of the multiplication.  c_t . h_t: every lane's term goes to LDS, lane j adds up token j's.
-// b and c of a tile lie in LDS as fp32.  With too few channels for the chip, tokens are cut into segments: what each leaves from
+// b and c of a tile lie in LDS as fp32.  A state goes over a tile by the tile's own factor (mdh_selective.h): in turn that is another
+// multiplication a step, the product of the factors that it went by (32768 tokens of 1536 channels 486 us, so 506).  With too few channels for the chip, tokens are cut into segments: what each leaves from
 // a state of zeros and the sum of its deltas (its decay is e^(A sum)), a prefix sum over the segments, the pass itself.
 #include "mdh_selective.h"
 
@@ -40,7 +41,7 @@ using ManyAtOnce = Form<NS, 8, 8, 128>;
 
 // STATES_ONLY: a segment's own state and sum of deltas.  Else the pass.
 template <typename T, int NS, typename F, bool STATES_ONLY>
-__global__ __launch_bounds__(F::THREADS) void scan_kernel(ScanCall c, Segments segs, int blocks) {
+__global__ __launch_bounds__(F::THREADS, NS == 4 ? 3 : 1) void scan_kernel(ScanCall c, Segments segs, int blocks) {
   constexpr int S = NS * 16, CH = F::CH, W = F::W, TOKENS = F::TOKENS, NA = STATES_ONLY ? 2 : 3, NB = STATES_ONLY ? 1 : 2;
   typedef Stage<T, NA, NB, CH, S, TOKENS, F::THREADS> In;
   typedef Outputs<T, 1, CH, TOKENS, F::THREADS> Out;
@@ -104,14 +105,17 @@ __global__ __launch_bounds__(F::THREADS) void scan_kernel(ScanCall c, Segments s
       const int at = place_of<T, CH>(i0 + p.j, p.row);
       const bool live = i0 + p.j < tokens;
       const Token k = token_of(c, to_float(xs[at]), to_float(dts[at]), live, dt_bias);
-      const float u = k.delta * k.x, grow = growth(k.delta, lane);
+      const float u = k.delta * k.x, sum = sum_of_row(k.delta);
       total += k.delta;
       float y[kTile];
       const float* bs = bc + p.j * In::kPitch + i0;
       if constexpr (W == 1) {
         keep(t0 + i0, h);
 #pragma unroll
-        for (int s = 0; s < NS; ++s)
+        for (int s = 0; s < NS; ++s) {
+          const float before = h[s];
+          float all = 1.f;
+          if (STATES_ONLY) h[s] = 0.f;
           unroll<kTile / 4>([&](auto quarter) {
             constexpr int Q = decltype(quarter)::value * 4;
             const Float4 bt = four_of(bs + s * 16 * In::kPitch + Q), ct = four_of(bs + (STATES_ONLY ? 0 : In::kFloats) + s * 16 * In::kPitch + Q);
@@ -119,11 +123,17 @@ __global__ __launch_bounds__(F::THREADS) void scan_kernel(ScanCall c, Segments s
               constexpr int I = decltype(i)::value;
               const float a = exp2_of(lane_of_row<Q + I>(k.delta) * A[s]);
               h[s] = fmaf(a, h[s], lane_of_row<Q + I>(u) * bt[I]);
-              if (!STATES_ONLY) y[Q + I] = s ? fmaf(ct[I], h[s], y[Q + I]) : ct[I] * h[s];
+              if (!STATES_ONLY) all *= a, y[Q + I] = s ? fmaf(ct[I], h[s], y[Q + I]) : ct[I] * h[s];
             });
           });
-#pragma unroll
-        for (int s = 0; s < NS; ++s) h[s] = fmaf(h[s], grow, h[s]);
+          const float factor = factor_of(sum, A[s]);
+          if (STATES_ONLY) {
+            h[s] = fmaf(factor, before, h[s]);
+          } else {
+            h[s] += put_right(factor, all, before);
+            if (NS == 4) settle(h[s]);  // (one block of states after the other: all at once take 191 registers for 149)
+          }
+        }
       } else {
         float own[NS][kTile], product[NS][kTile];
 #pragma unroll
@@ -140,7 +150,7 @@ __global__ __launch_bounds__(F::THREADS) void scan_kernel(ScanCall c, Segments s
               own[s][Q + I] = from_zero, product[s][Q + I] = all;
             });
           });
-          ends[tile][(s * CH + p.row) * 16 + p.j] = make_float2(from_zero, fmaf(all, grow, all));
+          ends[tile][(s * CH + p.row) * 16 + p.j] = make_float2(from_zero, factor_of(sum, A[s]));
         }
         __syncthreads();
         float before[NS];

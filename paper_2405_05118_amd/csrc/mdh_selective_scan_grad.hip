@@ -2,7 +2,7 @@
 //   G_t = E_t + d_p c_t,  E_{t-1} = a_t G_t;   d_c = sum_d d_p h_t,  d_b = sum_d G_t delta x,  r = sum_n G_t b_t,  q = G_t a_t h_{t-1}
 //   d_x = delta r + skip d_p,  d_delta = sum_n q A + x r,  d_A = sum_t q delta,  d_skip = sum d_p x,  d_gate = d_y p silu'(gate)
 // from the last token to the first.  The states h come from the forward call's checkpoints, one for every tile of 16 tokens:
-// a tile's a_t and h_t are computed again and stay in registers while it is walked back.
+// a tile's a_t and h_t are computed again and stay in registers while it is walked back; E goes over the tile by the tile's own factor.
 //
 // 1 exponential and 15 multiplications a step: bound by the vector ALU (26 of its instructions a step, sums and staging with them).
 // 4 x 2048 tokens of 4096 channels with 16 states, bf16: 516 to 565 us in a kernel trace, 26 for the sums of d_b and d_c.
@@ -68,18 +68,19 @@ __global__ __launch_bounds__(kThreads) void grad_segments_kernel(ScanCall c, Par
       float dp = to_float(dys[at]);
       if (c.in[2].p) dp *= gate_of(to_float(gates[at]));
       total += k.delta;
-      const float grow = growth(k.delta, threadIdx.x & 63);
+      const float sum = sum_of_row(k.delta);
 #pragma unroll
       for (int s = 0; s < NS; ++s) {
+        float own = 0.f;
         unroll<kTile / 4>([&](auto quarter) {
           constexpr int Q = kTile - 4 - decltype(quarter)::value * 4;
           const Float4 ct = four_of(cs + (s * 16 + p.j) * In::kPitch + i0 + Q);
           unroll<4>([&](auto i) {
             constexpr int I = 3 - decltype(i)::value;
-            e[s] = exp2_of(lane_of_row<Q + I>(k.delta) * A[s]) * fmaf(lane_of_row<Q + I>(dp), ct[I], e[s]);
+            own = exp2_of(lane_of_row<Q + I>(k.delta) * A[s]) * fmaf(lane_of_row<Q + I>(dp), ct[I], own);
           });
         });
-        e[s] = fmaf(e[s], grow, e[s]);
+        e[s] = fmaf(factor_of(sum, A[s]), e[s], own);
       }
     }
     __syncthreads();
@@ -173,13 +174,13 @@ __global__ __launch_bounds__(64 * WAVES, NS == 1 && sizeof(T) == 2 ? 4 : 2) void
       const int at = place_of<T, CH>(i0 + p.j, p.row);
       const Token k = token_of(c, to_float(xs[at]), to_float(dts[at]), live, dt_bias);
       const float dy = to_float(dys[at]), dp = c.in[2].p ? dy * gate_of(to_float(gates[at])) : dy, u = k.delta * k.x;
-      const float grow = growth(k.delta, lane);
+      const float delta_sum = sum_of_row(k.delta);
       float sp = 0.f, sr = 0.f, sq = 0.f;
       float* own = sums[wave];
 #pragma unroll
       for (int s = 0; s < NS; ++s) {
         const float* bs = bc + (s * 16 + p.j) * In::kPitch + i0;
-        float h[kTile + 1], a[kTile], g[kTile];
+        float h[kTile + 1], a[kTile], g[kTile], all = 1.f;
         h[0] = h0[tile][s];
         unroll<kTile / 4>([&](auto quarter) {
           constexpr int Q = decltype(quarter)::value * 4;
@@ -187,10 +188,13 @@ __global__ __launch_bounds__(64 * WAVES, NS == 1 && sizeof(T) == 2 ? 4 : 2) void
           unroll<4>([&](auto i) {
             constexpr int I = Q + decltype(i)::value;
             a[I] = exp2_of(lane_of_row<I>(k.delta) * A[s]);
+            all *= a[I];
             h[I + 1] = fmaf(a[I], h[I], lane_of_row<I>(u) * bt[I - Q]);
             own[I * kSumPitch + lane] = ct[I - Q] * h[I + 1];
           });
         });
+        float right = put_right(factor_of(delta_sum, A[s]), all, e[s]);
+        settle(right);
         wave_fence();
         sp += row_sum(own, lane);
         settle(sp);
@@ -221,7 +225,7 @@ __global__ __launch_bounds__(64 * WAVES, NS == 1 && sizeof(T) == 2 ? 4 : 2) void
             add_lane_of_row<I>(dA[s], delta2, a[I]);
           });
         });
-        e[s] = fmaf(e[s], grow, e[s]);
+        e[s] += right;
         wave_fence();
         sr += row_sum(own, lane);
         settle(sr), settle(dA[s]), settle(e[s]);

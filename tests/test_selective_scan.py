@@ -204,6 +204,55 @@ def test_slow_decays_add_up_no_bias(dtype, B, T, D, N):
         assert off <= T / 16 + 2 * np.sqrt(T / N) + 32, "%s: %.0f" % (what, off)
 
 
+# in turn (two kinds), 4 tiles at once (two kinds), 8 at once, segments
+FORMS = [(4, 8192, 4096, 8), (1, 8192, 8192, 40), (1, 5800, 4096, 16), (1, 5800, 4096, 24), (1, 2500, 2048, 16), (1, 32768, 64, 16), (1, 16000, 4096, 16)]
+
+
+def _through(dtype, B, T, D, N, delta, A, h0):
+    """What is left of the states h0 after T tokens that add nothing, and of such gradients of the final states."""
+    x, dt = torch.zeros(B, T, D, dtype=dtype, device="cuda"), delta.to(dtype).cuda()[None, :, None].expand(B, T, D).contiguous()
+    b, end, begin = torch.zeros(B, T, 1, N, dtype=dtype, device="cuda"), torch.empty_like(h0), torch.empty_like(h0)
+    sizes = (B, T, D, N, 1)
+    kept = torch.empty(mdh.mdh_selective_scan_checkpoints_size(sizes), dtype=torch.uint8, device="cuda")
+    ws = torch.empty(mdh.mdh_selective_scan_workspace_size(sizes, dtype, True), dtype=torch.uint8, device="cuda")
+    mdh.mdh_selective_scan(x, dt, A, b, b, torch.empty_like(x), initial_state=h0, final_state=end, checkpoints=kept, workspace=ws)
+    mdh.mdh_selective_scan_backward(x, dt, A, b, b, x, torch.empty_like(x), torch.empty_like(x), torch.empty_like(A), torch.empty_like(b),
+                                    torch.empty_like(b), kept, d_final_state=h0, d_initial_state=begin, workspace=ws)
+    return (end, "end"), (begin, "begin")
+
+
+@gpu
+@pytest.mark.parametrize("dtype", [F32, BF16])
+@pytest.mark.parametrize("B,T,D,N", FORMS)
+def test_states_without_decay_stay(dtype, B, T, D, N):
+    """A = 0: the factor is 1 whatever the time steps are, and the state's bits are those that came in."""
+    h0 = rand(1, B, D, N).cuda()
+    for got, what in _through(dtype, B, T, D, N, torch.rand(T, generator=torch.Generator().manual_seed(2)), torch.zeros(D, N, device="cuda"), h0):
+        assert torch.equal(got, h0), what
+
+
+@gpu
+@pytest.mark.parametrize("dtype", [F32, BF16])
+@pytest.mark.parametrize("steps", ["near 0", "one of sixteen"])
+@pytest.mark.parametrize("B,T,D,N", FORMS)
+def test_time_steps_near_zero(dtype, steps, B, T, D, N):
+    """Tokens to be ignored: time steps of 2^-30 to 2^-28, whose factors are 1 in 32 bits, alone or around a token of about 2^-9 in every
+    tile.  h_T = h_0 e^(A sum of delta), and its gradient is the same.  A tile of ignored tokens: the state is rounded by u at most, its factor by
+    0.7 u, with 0.12 u of the exponent's shift.  Where one of sixteen moves it, errors are of random sign but for less than u a tile: in
+    the mean over the states T u / 16, and four times the square root of T / 4 N."""
+    r = torch.Generator().manual_seed(3)
+    delta = torch.rand(T, generator=r) * 2.0 ** -29 + 2.0 ** -30
+    if steps == "one of sixteen":
+        delta = torch.where(torch.arange(T) % 16 == 5, torch.rand(T, generator=r) * 2.0 ** -9 + 2.0 ** -10, delta)
+    A, h0 = -1 - torch.rand(D, N, generator=r), (1 + torch.rand(B, D, N, generator=r)).cuda()
+    want = np.exp(np64(A) * np64(delta.to(dtype)).sum())
+    for got, what in _through(dtype, B, T, D, N, delta, A.cuda(), h0):
+        off = (np64(got) / np64(h0) / want - 1) / U
+        worst = np.abs(off).max() if steps == "near 0" else np.abs(off.mean(axis=-1)).max()
+        limit = 1.9 * T / 16 + 32 if steps == "near 0" else T / 16 + 2 * np.sqrt(T / N) + 32
+        assert worst <= limit, "%s: %.0f of %.0f" % (what, worst, limit)
+
+
 @gpu
 @pytest.mark.parametrize("dtype", [F32, BF16])
 def test_strides(dtype):
