@@ -643,7 +643,7 @@ mdh_status mdh_causal_conv_step(const int64_t* sizes, mdh_dtype dtype, const voi
 
 /*
  * The selective state space scan.  For every batch entry b, channel ch (of group g = ch / (D / G)) and state n < N:
- *   delta_t = softplus(dt_t + dt_bias)           (softplus = 0: dt_t + dt_bias itself)
+ *   delta_t = softplus(dt_t + dt_bias)           (softplus = 0: dt_t + dt_bias itself; softplus(-infinity) = 0: the state stays)
  *   h_t[n] = exp(delta_t A[ch][n]) h_{t-1}[n] + delta_t x_t b_t[g][n]
  *   y_t = (sum_n c_t[g][n] h_t[n] + skip[ch] x_t) silu(gate_t)          for t < lengths[b]
  * -- the prefix-sum operator on pairs, (a1, u1) op (a2, u2) = (a1 a2, a2 u1 + u2) (paper: Appendix, Example "Prefix-Sum"), with a

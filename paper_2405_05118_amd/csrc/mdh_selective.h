@@ -65,11 +65,11 @@ __device__ __forceinline__ float put_right(float factor, float product, float be
   return (factor - product) * __builtin_amdgcn_fmed3f(before, -3e38f, 3e38f);
 }
 
-// e^v with the rounding of v log2(e) put right
+// e^v with the rounding of v log2(e) put right (0 and infinity stay: v log2(e) may be infinite there, and its rounding NaN)
 __device__ __forceinline__ float exp_of(float v) {
   const float p = v * kLog2e, r = fmaf(v, kLog2e, -p) + v * 1.92596299e-8f;  // log2(e) = kLog2e + 1.926e-8
   const float e = exp2_of(p);
-  return e < 3e38f ? fmaf(e, r * kLn2, e) : e;
+  return e > 0.f && e < 3e38f ? fmaf(e, r * kLn2, e) : e;
 }
 // log(1 + e^v).  log(1 + e) = 2 artanh(e / (2 + e)), whose series of five terms is off by less than 2^-26 up to e = 0.4
 // (s = 1/6: s^10 / 11); beyond, 1 + e is rounded by 2^-24 of a logarithm above 0.33.

@@ -166,6 +166,39 @@ def test_time_steps_of_zero_and_of_thousands(dtype):
 
 @gpu
 @pytest.mark.parametrize("dtype", [F32, BF16])
+@pytest.mark.parametrize("mask", ["-inf", "lowest"])
+@pytest.mark.parametrize("B,T,D,N,G", [(2, 50, 20, 16, 2), (1, 40, 18, 40, 1), (1, 1300, 20, 16, 1)])
+def test_masked_time_steps(dtype, mask, B, T, D, N, G):
+    """Tokens whose dt is -infinity or the type's lowest value, which softplus makes 0: the state stays, dt's gradient is 0."""
+    low = -float("inf") if mask == "-inf" else torch.finfo(dtype).min
+    p = Problem(dtype, B, T, D, N, G)
+    p.dt[:, ::3], p.dt[:, 17:38, :5] = low, low
+    p.check()
+    assert not p.backward()[1][:, ::3].any()
+    p.dt[:] = low
+    p.check()
+    assert torch.equal(p.forward()[1].cpu(), p.h0)
+
+
+@gpu
+@pytest.mark.parametrize("dtype", [F32, BF16])
+@pytest.mark.parametrize("low", [-float("inf"), None])
+@pytest.mark.parametrize("N", [16, 18])
+def test_step_with_a_masked_time_step(dtype, low, N):
+    p = Problem(dtype, 3, 1, 30, N)
+    p.dt[1], p.dt[2, :, :7] = (torch.finfo(dtype).min if low is None else low,) * 2
+    a, k = p.oracle()
+    (ry, rf), (my, mf) = O.selective_scan(*a, **k), O.selective_scan(*a, **k, magnitude=True)
+    state, y = p.h0.cuda(), p.empty(3, 30)
+    mdh.mdh_selective_scan_step(*(t[:, 0].cuda() if t is not p.A else t.cuda() for t in (p.x, p.dt, p.A, p.b, p.c)), state, y, p.skip.cuda(),
+                                p.gate[:, 0].cuda(), p.dt_bias.cuda(), True)
+    close(y, ry[:, 0], my[:, 0], dtype == BF16, N + 503, "y")
+    close(state, rf, mf, False, 503, "state")
+    assert torch.equal(state[1].cpu(), p.h0[1]) and torch.equal(state[2, :7].cpu(), p.h0[2, :7])
+
+
+@gpu
+@pytest.mark.parametrize("dtype", [F32, BF16])
 @pytest.mark.parametrize("B,T,D,N,G", [(1, 2500, 8, 16, 1), (2, 1111, 20, 7, 2), (1, 1300, 33, 40, 1)])
 def test_long_sequences(dtype, B, T, D, N, G):
     """Long enough that one channel's tokens are worked on in several places at once."""
