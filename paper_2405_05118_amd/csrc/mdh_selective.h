@@ -44,6 +44,12 @@ __device__ __forceinline__ float again(float v) {
 // 2^x by the hardware (1 ulp; 0 below 2^-126)
 __device__ __forceinline__ float exp2_of(float x) { return __builtin_amdgcn_exp2f(x); }
 
+// A for powers of 2.  The largest numbers stay as they are: infinite, they would make NaN of a time step of 0.  (NaN stays, too.)
+__device__ __forceinline__ float in_powers_of_2(float A) {
+  const float v = A * kLog2e;
+  return v < -3.4e38f || v > 3.4e38f ? A : v;
+}
+
 // A state that decays slowly multiplies thousands of factors just below 1, each of them rounded, and v_exp_f32 is besides too small by
 // 0.12 2^-24 on average there (a million arguments from -1e-2 to -1e-5; no more than 0.7 2^-24 at any).  So a state goes over a tile of
 // tokens by the factor of the tile, e^(A sum of deltas), one exponential for 16 tokens: what the tokens' own factors are off by does not

@@ -66,7 +66,7 @@ __global__ __launch_bounds__(F::THREADS, NS == 4 ? 3 : 1) void scan_kernel(ScanC
   for (int s = 0; s < NS; ++s) {
     const int n = s * 16 + p.j;
     const bool has = mine && n < c.N;
-    A[s] = has ? c.A[d * c.N + n] * kLog2e : 0.f;
+    A[s] = has ? in_powers_of_2(c.A[d * c.N + n]) : 0.f;
     h[s] = 0.f;
     if (!STATES_ONLY && has) {
       if (segs.n > 1)
@@ -226,14 +226,14 @@ __global__ __launch_bounds__(256) void segments_kernel(ScanCall c, Segments segs
   const int64_t per = (int64_t)c.D * c.N, i = (int64_t)blockIdx.x * 256 + threadIdx.x;
   if (i >= c.B * per) return;
   const int64_t b = i / per, dn = i % per, d = dn / c.N, slot = rev ? b : scan_slot(c, b);
-  const float A = c.A[dn] * kLog2e;
+  const float A = in_powers_of_2(c.A[dn]);
   float h = start && slot >= 0 ? start[slot * per + dn] : 0.f;
   for (int k = 0; k < segs.n; ++k) {
     const int64_t seg = b * segs.n + (rev ? segs.n - 1 - k : k);
     float* at = segs.h + seg * per + dn;
     const float own = *at;
     *at = h;
-    h = fmaf(exp2_of(A * segs.sum[seg * c.D + d]), h, own);
+    h = fmaf(exp2_of(A * __builtin_amdgcn_fmed3f(segs.sum[seg * c.D + d], -3e38f, 3e38f)), h, own);  // (infinite times 0 is NaN)
   }
 }
 
@@ -257,7 +257,7 @@ __global__ __launch_bounds__(256) void scan_step_kernel(ScanCall c, unsigned blo
       const int g = (int)(d / (unsigned)c.E);
       float* state = c.s_out + (slot * c.D + d) * c.N + n;
       fv h = *(const fv*)state;
-      const fv A = *(const fv*)(c.A + (int64_t)d * c.N + n) * kLog2e;
+      const fv A = *(const fv*)(c.A + (int64_t)d * c.N + n);
       const T *pb = at<T>(c.bc[0], b, 0, g, n), *pc = at<T>(c.bc[1], b, 0, g, n);
       float bt[V], ct[V];
       if constexpr (V == 4) {
@@ -269,7 +269,7 @@ __global__ __launch_bounds__(256) void scan_step_kernel(ScanCall c, unsigned blo
       const Token k = token_of(c, x, dt, true, c.dt_bias ? c.dt_bias[d] : 0.f);
 #pragma unroll
       for (int s = 0; s < V; ++s) {
-        h[s] = fmaf(factor_of(k.delta, A[s]), h[s], k.delta * k.x * bt[s]);
+        h[s] = fmaf(factor_of(k.delta, in_powers_of_2(A[s])), h[s], k.delta * k.x * bt[s]);
         y = fmaf(ct[s], h[s], y);
       }
       *(fv*)state = h;

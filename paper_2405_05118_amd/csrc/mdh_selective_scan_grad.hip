@@ -53,7 +53,7 @@ __global__ __launch_bounds__(kThreads) void grad_segments_kernel(ScanCall c, Par
   float A[NS], e[NS], total = 0.f;
 #pragma unroll
   for (int s = 0; s < NS; ++s) {
-    A[s] = mine && s * 16 + p.j < c.N ? c.A[d * c.N + s * 16 + p.j] * kLog2e : 0.f;
+    A[s] = mine && s * 16 + p.j < c.N ? in_powers_of_2(c.A[d * c.N + s * 16 + p.j]) : 0.f;
     e[s] = 0.f;
   }
   const float dt_bias = mine && c.dt_bias ? c.dt_bias[d] : 0.f;
@@ -131,7 +131,7 @@ __global__ __launch_bounds__(64 * WAVES, NS == 1 && sizeof(T) == 2 ? 4 : 2) void
   for (int s = 0; s < NS; ++s) {
     const int n = s * 16 + p.j;
     const bool has = mine && n < c.N;
-    A[s] = has ? c.A[d * c.N + n] * kLog2e : 0.f;
+    A[s] = has ? in_powers_of_2(c.A[d * c.N + n]) : 0.f;
     e[s] = dA[s] = 0.f;
     if (has && w.n > 1)
       e[s] = w.e[(seg * c.D + d) * c.N + n];

@@ -199,6 +199,30 @@ def test_step_with_a_masked_time_step(dtype, low, N):
 
 @gpu
 @pytest.mark.parametrize("dtype", [F32, BF16])
+@pytest.mark.parametrize("B,T,D,N,G", [(2, 50, 20, 18, 2), (1, 40, 18, 40, 1), (1, 1300, 20, 16, 1), (3, 1, 30, 16, 1), (3, 1, 30, 18, 1)])
+def test_largest_time_steps_and_decays(dtype, B, T, D, N, G):
+    """Time steps and decays of the largest numbers: a token that resets all states but those without decay, states that live for one token
+    only or for those with a time step of 0."""
+    p = Problem(dtype, B, T, D, N, G)
+    p.dt[:, 5::11], p.dt[:, ::4] = torch.finfo(dtype).max, -float("inf")
+    p.x[:, 5::11] = 0
+    p.A[:, 0], p.A[3] = 0.0, torch.finfo(F32).min
+    p.check(backward=False)
+    p.A[6, 1] = NAN  # (weights that are no numbers show)
+    assert p.forward()[0][..., 6].isnan().all()
+    p.A[6, 1] = -1.0
+    if T == 1:
+        a, k = p.oracle()
+        (ry, rf), (my, mf) = O.selective_scan(*a, **k), O.selective_scan(*a, **k, magnitude=True)
+        state, y = p.h0.cuda(), p.empty(B, D)
+        mdh.mdh_selective_scan_step(*(t[:, 0].cuda() if t is not p.A else t.cuda() for t in (p.x, p.dt, p.A, p.b, p.c)), state, y, p.skip.cuda(),
+                                    p.gate[:, 0].cuda(), p.dt_bias.cuda(), True)
+        close(y, ry[:, 0], my[:, 0], dtype == BF16, N + 503, "y")
+        close(state, rf, mf, False, 503, "state")
+
+
+@gpu
+@pytest.mark.parametrize("dtype", [F32, BF16])
 @pytest.mark.parametrize("B,T,D,N,G", [(1, 2500, 8, 16, 1), (2, 1111, 20, 7, 2), (1, 1300, 33, 40, 1)])
 def test_long_sequences(dtype, B, T, D, N, G):
     """Long enough that one channel's tokens are worked on in several places at once."""
