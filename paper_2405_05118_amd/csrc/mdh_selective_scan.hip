@@ -301,6 +301,7 @@ Plan plan(const ScanCall& c) {
   const int ns = states_of(c);
   const int64_t T = c.T, eights = c.B * c.G * cdiv(c.E, 8), groups = c.B * c.G * cdiv(c.E, 16);
   const int64_t turn = T * (55 + (groups <= 256 ? 60 : groups * 60 / 256)), four = T * (eights <= 256 ? 65 : 98 * cdiv(eights, 512)), eight = T * 60 * cdiv(eights, 256);
+  if (groups == 0) return {1, 1, T};  // (no sequences: no channels to share segments out over)
   const int64_t cut = T * groups * 92 / 256 + 36000;
   Plan z{1, 1, 0};
   int64_t best = turn;

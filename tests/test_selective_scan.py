@@ -635,6 +635,16 @@ def test_refusals():
     assert step((2, 8, 16, 1), x=None) == E_NULL and step((2, 8, 16, 1), state=None) == E_NULL and step((0, 8, 16, 1)) == 0
 
 
+@pytest.mark.parametrize("T", [0, 313, 314, 1024, 100000])
+@pytest.mark.parametrize("N", [16, 17, 33, 64])
+def test_an_empty_batch_wants_no_workspace(T, N):
+    for dtype in (F32, BF16):
+        for D, G in ((256, 1), (16, 16)):
+            sizes = (0, T, D, N, G)
+            assert mdh.mdh_selective_scan_workspace_size(sizes, dtype) == 0 == mdh.mdh_selective_scan_workspace_size(sizes, dtype, True)
+            assert mdh.mdh_selective_scan_checkpoints_size(sizes) == 0
+
+
 def test_refuses_gradients_of_b_and_c_past_2_31_elements():
     assert _back((1, 17, 3900000, 64, 3900000)) == E_SIZE and _back((1, 1 << 21, 64, 64, 16)) == E_SIZE
 
