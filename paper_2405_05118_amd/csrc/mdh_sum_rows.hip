@@ -7,17 +7,18 @@ namespace mdh {
 namespace {
 
 constexpr int kTeams = 16;
+constexpr int64_t kColumns = (int64_t)1 << 27;  // of a launch: 2^31 lanes
 
 struct SumArgs {
   const float* part;
-  int64_t rows, n;
+  int64_t rows, n, first;  // columns, the launch's first one
   SumTarget to[3];
 };
 
 __global__ __launch_bounds__(64 * kTeams) void sum_rows_kernel(SumArgs s) {
   __shared__ float sums[kTeams][64];
   const int lane = threadIdx.x & 63, team = threadIdx.x >> 6;
-  int64_t col = (int64_t)blockIdx.x * 64 + lane;
+  int64_t col = s.first + (int64_t)blockIdx.x * 64 + lane;
   float x[4] = {0.f, 0.f, 0.f, 0.f};
   if (col < s.n) {
     const float* p = s.part + col;
@@ -43,12 +44,15 @@ __global__ __launch_bounds__(64 * kTeams) void sum_rows_kernel(SumArgs s) {
 }  // namespace
 
 mdh_status launch_sum_rows(const float* part, int64_t rows, int64_t n, const SumTarget (&to)[3], hipStream_t st) {
-  if (n == 0) return MDH_OK;
-  if (cdiv(n, 64) * 64 * kTeams >= (int64_t)1 << 32) return MDH_ERR_SIZE;
-  const SumArgs s{part, rows, n, {to[0], to[1], to[2]}};
+  if (!to[0].p && !to[1].p && !to[2].p) return MDH_OK;
   clear_stale_error();
-  sum_rows_kernel<<<(unsigned)cdiv(n, 64), 64 * kTeams, 0, st>>>(s);
-  return launch_status();
+  for (int64_t first = 0; first < n; first += kColumns) {
+    const SumArgs s{part, rows, n, first, {to[0], to[1], to[2]}};
+    sum_rows_kernel<<<(unsigned)cdiv(n - first < kColumns ? n - first : kColumns, 64), 64 * kTeams, 0, st>>>(s);
+    const mdh_status r = launch_status();
+    if (r != MDH_OK) return r;
+  }
+  return MDH_OK;
 }
 
 }  // namespace mdh

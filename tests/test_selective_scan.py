@@ -461,6 +461,36 @@ def test_activations_past_2_31_elements():
 
 
 @gpu
+def test_gradients_of_more_parameters_than_a_launch_has_lanes():
+    """4 million channels with 64 states: d_A, d_skip and d_dt_bias are 277 million sums over the sequences.  A channel's are those of a
+    call on some channels alone, bit for bit."""
+    B, D, N = 2, 1 << 22, 64
+    r = torch.Generator("cuda").manual_seed(1)
+    new = lambda *shape: torch.randn(shape, generator=r, device="cuda")  # noqa: E731
+    x, dt, d_y, b, c, A, dh = new(B, 1, D), new(B, 1, D), new(B, 1, D), new(B, 1, 1, N), new(B, 1, 1, N), -new(D, N).abs(), new(B, D, N)
+
+    def grads(*channels):
+        """[d_A, d_skip, d_dt_bias] of a range of channels"""
+        p, q, w, a, g = (t[..., slice(*channels)].contiguous() for t in (x, dt, d_y, A.T, dh.transpose(1, 2)))
+        a, g = a.T.contiguous(), g.transpose(1, 2).contiguous()
+        n = a.shape[0]
+        sizes = (B, 1, n, N, 1)
+        kept = torch.empty(mdh.mdh_selective_scan_checkpoints_size(sizes), dtype=torch.uint8, device="cuda")
+        ws = torch.empty(mdh.mdh_selective_scan_workspace_size(sizes, F32, True), dtype=torch.uint8, device="cuda")
+        out = [torch.full(s, NAN, device="cuda") for s in ((n, N), (n,), (n,))]
+        mdh.mdh_selective_scan(p, q, a, b, c, torch.empty_like(p), initial_state=g, checkpoints=kept, workspace=ws, softplus=True)
+        mdh.mdh_selective_scan_backward(p, q, a, b, c, w, torch.empty_like(p), torch.empty_like(p), out[0], torch.empty_like(b), torch.empty_like(b),
+                                        kept, d_final_state=g, d_skip=out[1], d_dt_bias=out[2], workspace=ws, softplus=True)
+        return out
+
+    got = grads(0, D)
+    assert torch.equal(got[1], d_y[0, 0] * x[0, 0] + d_y[1, 0] * x[1, 0])
+    for lo in (0, (1 << 21) - 50, D - 100):
+        for whole, part in zip(got, grads(lo, lo + 100)):
+            assert torch.equal(whole[lo:lo + 100], part), lo
+
+
+@gpu
 def test_prompt_then_tokens():
     """A prompt and the tokens after it, one at a time, are one sequence."""
     p = Problem(F32, 2, 60, 40, 16, 2)
