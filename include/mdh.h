@@ -605,7 +605,8 @@ mdh_status mdh_group_norm_backward(const int64_t* sizes, mdh_dtype dtype, const 
  *   sizes    (B, T, C, W): 0 <= B, 0 <= T < 2^31 - 64, B * T < 2^31, 1 <= C < 2^24, 1 <= W <= 8 (MDH_ERR_UNSUPPORTED).
  *            A call has fewer than 2^24 workgroups of 256 lanes (MDH_ERR_SIZE), a lane for 4 channels of 8 to 64 tokens.
  *   x, y     (B, T, C) of type dtype; strides: 4 numbers, (batch, token) of x, y in elements, channels adjacent;
- *            NULL: dense.  Any alignment that the type has.  y does not overlap x.
+ *            NULL: dense.  Any alignment that the type has.  y does not overlap x; y = x is refused (MDH_ERR_UNSUPPORTED)
+ *            where W > 1.
  *   weight   (C, W) fp32; bias: C fp32 or NULL (zeros); act: MDH_ACT_*
  *   lengths  B int32 or NULL (all T).  Tokens from lengths[b] on are not read (any value, NaN too); their outputs
  *            are 0.  Less than 0 counts as 0, more than T as T.
@@ -620,7 +621,8 @@ mdh_status mdh_causal_conv(const int64_t* sizes, mdh_dtype dtype, const void* x,
                            void* final_window, const int32_t* slots, int64_t n_slots, void* y, void* stream);
 /*
  * Gradients of mdh_causal_conv from those of y and of the final window (NULL: zeros).
- *   strides  6 numbers, (batch, token) of x, d_y, d_x; NULL: dense.  d_x does not overlap x or d_y.
+ *   strides  6 numbers, (batch, token) of x, d_y, d_x; NULL: dense.  d_x does not overlap x or d_y; in place of either it is
+ *            refused where W > 1.
  *   initial_window  what the forward call had (without slots); d_initial_window: NULL = not wanted
  *   d_weight, d_bias  (C, W) and C fp32 or NULL; summed over all tokens in a fixed order
  *   workspace  mdh_causal_conv_workspace_size(sizes, dtype) bytes, 16-byte aligned

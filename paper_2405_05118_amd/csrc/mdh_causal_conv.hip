@@ -325,6 +325,11 @@ mdh_status launch(const ConvCall& c, Which which, hipStream_t st) {
   const Grid g = grid_of(c, which);
   const int64_t blocks = g.blocks * g.groups * c.B;
   if (blocks >= 1 << 24) return MDH_ERR_SIZE;  // 2^32 lanes
+  // a run reads the last rows of the run before it, which are another lane's to write
+  if (c.W > 1 && c.T > 0 && which != kStep) {
+    const bool here = which == kForward ? c.y.p == c.x.p : c.dx.p == c.x.p || c.dx.p == c.y.p;
+    if (here) return MDH_ERR_UNSUPPORTED;
+  }
   clear_stale_error();
   if (c.dtype == MDH_BF16)
     taps_of<bf16>(c, which, g, (unsigned)blocks, st);

@@ -327,6 +327,27 @@ def test_refuses_outputs_whose_rows_overlap():
     assert _back(ok, strides=[80, 16, 80, 16, 80, 15]) == E_SIZE and _back(ok, strides=[80, 16, 80, 16, 15, 16]) == E_SIZE
 
 
+def test_refuses_outputs_in_place():
+    """A run of tokens reads rows of the one before it: y where x is, d_x where x or d_y is."""
+    ok = (2, 500, 16, 4)
+    for sizes in (ok, (1, 1, 1, 2), (2, 500, 16, 8)):
+        for dtype in (0, 1):
+            assert _raw(sizes, dtype=dtype, x=64, y=64) == E_UNSUP
+        assert _back(sizes, x=64, d_y=128, d_x=64) == E_UNSUP and _back(sizes, x=64, d_y=128, d_x=128) == E_UNSUP
+    wide = [500 * 40, 40] * 3
+    assert _raw(ok, strides=wide[:4]) == E_UNSUP and _back(ok, strides=wide) == E_UNSUP
+    assert _raw((2, 0, 16, 4)) == 0 and _raw((0, 5, 16, 4)) == 0  # no tokens
+
+
+@gpu
+@pytest.mark.parametrize("dtype", [F32, BF16])
+def test_one_tap_in_place(dtype):
+    p = Problem(dtype, 2, 300, 40, 1, windows=False)
+    y, here = p.forward()[0], p.x.cuda()
+    mdh.mdh_causal_conv(here, p.w.cuda(), p.b.cuda(), here, mdh.MDH_ACT_SILU)
+    assert torch.equal(here, y)
+
+
 def test_refusals():
     ok = (2, 5, 16, 4)
     for sizes in ((-1, 5, 16, 4), (2, -1, 16, 4), (2, 5, 0, 4), (2, 5, 16, 0), (1 << 16, 1 << 16, 16, 4), (2, 5, 1 << 24, 4), (1, (1 << 31) - 1, 8, 4)):
