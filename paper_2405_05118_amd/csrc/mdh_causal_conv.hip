@@ -182,16 +182,21 @@ __global__ __launch_bounds__(kThreads) void conv_backward_kernel(ConvCall c, Gri
         const float zero[V] = {};
         shift<W, V>(open, zero);
         const bool live = t + u < p.len, own = t + u < t1;
+        float dz[V];
 #pragma unroll
         for (int i = 0; i < V; ++i) {
-          const float dz = live ? dy[i] * slope[i] : 0.f, mine = own ? dz : 0.f;
+          dz[i] = live ? dy[i] * slope[i] : 0.f;
 #pragma unroll
-          for (int j = 0; j < W; ++j) {
-            open[j][i] = fmaf(w[j][i], dz, open[j][i]);
-            dw[j][i] = fmaf(mine, window[j][i], dw[j][i]);
-          }
-          db[i] += mine;
+          for (int j = 0; j < W; ++j) open[j][i] = fmaf(w[j][i], dz[i], open[j][i]);
         }
+        // (0 times a window that no valid token reads, one before a sequence of no tokens, may be NaN)
+        if (live && own)
+#pragma unroll
+          for (int i = 0; i < V; ++i) {
+#pragma unroll
+            for (int j = 0; j < W; ++j) dw[j][i] = fmaf(dz[i], window[j][i], dw[j][i]);
+            db[i] += dz[i];
+          }
         const int64_t s = t + u - (W - 1);  // complete now
         if (s < first) continue;
         const int64_t tail = s - (p.len - (W - 1));  // row of the window that went out

@@ -131,6 +131,23 @@ def test_lengths_with_anything_behind_them(dtype, lengths):
 
 @gpu
 @pytest.mark.parametrize("dtype", [F32, BF16])
+@pytest.mark.parametrize("bad", [NAN, float("inf")])
+@pytest.mark.parametrize("W", [2, 4, 8])
+def test_what_no_token_reads_is_in_no_gradient(dtype, bad, W):
+    """The window before a sequence of no tokens, and a last token for all taps but its own."""
+    p = Problem(dtype, 3, 200, 21, W, "none", lengths=[200, 0, 77])
+    p.before[1], p.x[0, 199, 3], p.x[2, 76, 5] = 0, 0, 0
+    d_x, d_w, d_b, d_before = p.backward()
+    p.before[1], p.x[0, 199, 3], p.x[2, 76, 5] = bad, bad, bad
+    got = p.backward()
+    assert torch.equal(got[0], d_x) and torch.equal(got[2], d_b) and torch.equal(got[3], d_before)
+    assert torch.equal(got[1][:, :-1], d_w[:, :-1])
+    rest = [i for i in range(21) if i not in (3, 5)]
+    assert torch.equal(got[1][rest], d_w[rest]) and not got[1][[3, 5], -1].isfinite().any()
+
+
+@gpu
+@pytest.mark.parametrize("dtype", [F32, BF16])
 @pytest.mark.parametrize("C", [24, 27])
 def test_strides(dtype, C):
     """Columns of wider rows, at odd places; one token's values for all tokens; what lies beside an output stays."""
