@@ -713,8 +713,9 @@ mdh_status mdh_selective_scan_step(const int64_t* sizes, mdh_dtype dtype, const 
  *            dense.  Any alignment that the type has.  residual: NULL, or total receives s (x, residual or a buffer of its own).
  *            y may be x where there is no residual.
  *   weight, bias  C fp32, or NULL (1 and 0);  mean, rstd: rows fp32 each, or NULL: what the backward call wants
- * Variances are sums of squared differences from the mean, in fp32; one value in all of a row gives bias.  Inf or NaN in a row
- * makes that row NaN and no other.
+ * Variances are sums of squared differences from the mean, in fp32; one value in all of a row gives bias, up to the largest one.
+ * Values some 2^64 apart, whose squares are not, have the variance infinity: rstd = 0.  Inf or NaN in a row makes that row NaN
+ * and no other.
  */
 mdh_status mdh_layer_norm(const int64_t* sizes, mdh_dtype dtype, const void* x, const void* residual, const int64_t* row_strides,
                           const float* weight, const float* bias, float eps, void* total, void* y, float* mean, float* rstd,

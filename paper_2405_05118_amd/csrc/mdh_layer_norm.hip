@@ -40,17 +40,34 @@ __device__ __forceinline__ void row_sums(float& a, float& b, int& turn) {
 struct Moments {
   float mean, rstd;
 };
-// from the sum of a row: `differ` gives the lane's sums of differences from a mean and of their squares
-template <int L, typename F>
-__device__ __forceinline__ Moments moments(float sum, int C, float eps, int& turn, F differ) {
+// from the sum of a row: `differ` gives the lane's sums of differences from a mean and of their squares, `scaled` that of its values
+// times a factor, for rows whose sum is past the largest number
+template <int L, typename F, typename G>
+__device__ __forceinline__ Moments moments(float sum, int C, float eps, int& turn, F differ, G scaled) {
+  constexpr float kLargest = 3.40282347e38f;
   float none = 0.f, d = 0.f, d2 = 0.f;
   row_sums<L>(sum, none, turn);
   const float over = 1.f / (float)C;
   float mean = sum * over;
+  if (!(fabsf(sum) <= kLargest)) {  // (the same for all lanes of the row)
+    float half = scaled(0.5f * over);
+    row_sums<L>(half, none, turn);
+    mean = fabsf(half) <= kLargest ? fminf(fmaxf(2.f * half, -kLargest), kLargest) : half;  // (infinity and NaN stay)
+  }
   asm("" : "+v"(mean));  // (rounded here: fused into the differences, it would be another number than the one that is put right)
   differ(mean, d, d2);
   row_sums<L>(d, d2, turn);
-  const float off = d * over, var = fmaxf(d2 * over - off * off, 0.f);
+  float off = d * over;
+  if (!(d2 <= kLargest)) {
+    // squares past the largest number: of values that far apart (a variance of infinity), or of what the mean's rounding came to, which
+    // is put right first
+    if (fabsf(off) <= kLargest) mean += off;
+    d = d2 = 0.f;
+    differ(mean, d, d2);
+    row_sums<L>(d, d2, turn);
+    off = 0.f;
+  }
+  const float var = fmaxf(d2 * over - off * off, 0.f);
   // (means within 16 times the spread are right as they are: the differences' own roundings would be added to them)
   if (mean * mean > 256.f * var) mean += off;
   // NaN and infinity stay: fmaxf would drop NaN
@@ -97,6 +114,13 @@ __global__ __launch_bounds__(L > 256 ? L : 256) void layer_norm_kernel(LayerNorm
           const float e = x[k][i] - mean;
           d += e, d2 = fmaf(e, e, d2);
         }
+  }, [&](float factor) {
+    float s = 0.f;
+#pragma unroll
+    for (int k = 0; k < P; ++k)
+#pragma unroll
+      for (int i = 0; i < V; ++i) s = fmaf(x[k][i], factor, s);
+    return s;
   });
   if (!live) return;
   if (l == 0) {
@@ -152,6 +176,15 @@ __global__ __launch_bounds__(kWide) void layer_norm_wide_kernel(LayerNormCall c)
           d += e, d2 = fmaf(e, e, d2);
         }
     }
+  }, [&](float factor) {
+    float s = 0.f;
+    for (int ch = threadIdx.x * V; ch < c.C; ch += kWide * V) {
+      float x[V];
+      unpack_row<T>(load_row<T>(at<T>(from, row, ch), c.C - ch), x);
+#pragma unroll
+      for (int i = 0; i < V; ++i) s = fmaf(x[i], factor, s);
+    }
+    return s;
   });
   if (threadIdx.x == 0) {
     if (c.mean) c.mean[row] = m.mean;

@@ -179,6 +179,25 @@ def test_one_value_a_row_whatever_it_is(dtype, C):
 
 @gpu
 @pytest.mark.parametrize("dtype", [F32, BF16])
+@pytest.mark.parametrize("C", [2, 24, 110, 1028, 4096, 16384, 20000])
+def test_rows_whose_sum_is_past_the_largest_number(dtype, C):
+    """One value in all of a row gives the bias up to the largest one; with both signs the mean is near 0 and nothing is NaN; infinities still
+    make their row NaN, and no other."""
+    big = torch.finfo(dtype).max
+    values = torch.tensor([big, -big, 1e38, -2.9e37, 3e35, 1.0, 1.0, 1.0]).to(dtype)
+    p = Problem(dtype, len(values), C, residual=False)
+    p.x = values[:, None].repeat(1, C)
+    p.x[5] = torch.where(torch.arange(C) < C // 2, big, -big)
+    p.x[6, C // 2], p.x[7, 0] = float("inf"), NAN
+    y, _, mean, rstd = p.forward()
+    assert torch.equal(mean[:5].cpu(), values[:5].float()) and torch.equal(y[:5].cpu(), p.b.to(dtype).expand(5, C))
+    assert torch.isfinite(rstd[:6]).all() and torch.isfinite(mean[5]) and y[6:].isnan().all()
+    # C products and sums of at most half of the largest number, off by u of that each; twice, for the half
+    assert abs(float(mean[5]) - np64(p.x[5]).mean()) <= 2 * 2 * C * U * big / 2
+
+
+@gpu
+@pytest.mark.parametrize("dtype", [F32, BF16])
 @pytest.mark.parametrize("C", [30, 600, 4000, 18000])
 def test_nan_and_infinity_stay_in_their_row(dtype, C):
     p = Problem(dtype, 7, C)
