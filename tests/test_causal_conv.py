@@ -253,6 +253,24 @@ def test_past_2_31_elements():
 
 
 @gpu
+def test_gradients_past_2_31_elements():
+    """Operands and gradients as columns of one buffer whose last tokens are past 2^31 elements: the bits of dense ones."""
+    T = 150
+    p = Problem(BF16, 2, T, 21, 4, lengths=[T, T - 9])
+    want = [*p.forward(), *p.backward()]
+    wide = torch.empty(2, T, (1 << 31) // T + 400, dtype=BF16, device="cuda")
+    assert wide[0].numel() > 1 << 31
+    columns = iter(range(3, 400, 30))
+
+    def lay(t):
+        at = next(columns)
+        return wide[:, :, at:at + 21].copy_(t)
+
+    for got, ref in zip([*p.forward(lay, lay(p.x)), *p.backward(lay, lay(p.x))], want):
+        assert torch.equal(got, ref)
+
+
+@gpu
 def test_prompt_then_tokens():
     """A prompt and the tokens after it, one at a time, are one sequence, bit for bit."""
     p = Problem(BF16, 2, 30, 40, 4)

@@ -240,6 +240,26 @@ def test_rows_past_2_31_elements():
 
 
 @gpu
+@pytest.mark.parametrize("C", [100, 20000])
+def test_gradients_of_rows_past_2_31_elements(C):
+    """Operands and gradients as columns of one buffer whose last rows are past 2^31 elements: the bits of dense ones."""
+    rows = 300
+    p = Problem(BF16, rows, C)
+    _, _, mean, rstd = p.forward()
+    want = p.backward(mean, rstd)
+    wide = torch.empty(rows, (1 << 31) // (rows - 20), dtype=BF16, device="cuda")
+    assert wide[:-19].numel() > 1 << 31
+    columns = iter(range(3, 6 * C, C + 5))
+
+    def lay(t):
+        at = next(columns)
+        return wide[:, at:at + C].copy_(t)
+
+    for got, ref in zip(p.backward(mean, rstd, lay, lay(p.x)), want):
+        assert torch.equal(got, ref)
+
+
+@gpu
 @pytest.mark.parametrize("dtype", [F32, BF16])
 def test_chip_full_of_work(dtype):
     """Every output with every compute unit busy, against 64 bits on the GPU; the same bits in three calls."""

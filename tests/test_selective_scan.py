@@ -461,6 +461,30 @@ def test_activations_past_2_31_elements():
 
 
 @gpu
+@pytest.mark.parametrize("T", [40, 700])
+def test_gradients_past_2_31_elements(T):
+    """All operands and gradients as columns of one buffer whose last tokens are past 2^31 elements: the bits of dense ones."""
+    p = Problem(BF16, 2, T, 20, 16, 2, lengths=[T, T - 9])
+    want = [*p.forward(), *p.backward()]
+    wide = torch.empty(2, T, (1 << 31) // T + 4000, dtype=BF16, device="cuda")  # (the first sequence's last tokens are past it, too)
+    assert wide[0].numel() > 1 << 31
+    columns = iter(range(3, 5000, 47))
+
+    def place(shape):
+        at, n = next(columns), int(np.prod(shape[2:]))
+        view = wide[:, :, at:at + n]
+        return view if len(shape) == 3 else view.unflatten(2, shape[2:])
+
+    def lay(t):
+        return place(t.shape).copy_(t)
+
+    y = place(p.x.shape)
+    out = {n: place((p.b if n in ("d_b", "d_c") else p.x).shape) for n in GRADS[:5]}
+    for got, ref in zip([*p.forward(lay, y), *p.backward(lay, out=out)], want):
+        assert torch.equal(got, ref)
+
+
+@gpu
 def test_gradients_of_more_parameters_than_a_launch_has_lanes():
     """4 million channels with 64 states: d_A, d_skip and d_dt_bias are 277 million sums over the sequences.  A channel's are those of a
     call on some channels alone, bit for bit."""
