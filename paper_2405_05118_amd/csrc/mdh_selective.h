@@ -51,22 +51,22 @@ __device__ __forceinline__ float in_powers_of_2(float A) {
 }
 
 // A state that decays slowly multiplies thousands of factors just below 1, each of them rounded, and v_exp_f32 is besides too small by
-// 0.12 2^-24 on average there (a million arguments from -1e-2 to -1e-5; no more than 0.7 2^-24 at any).  So a state goes over a tile of
-// tokens by the factor of the tile, e^(A sum of deltas), one exponential for 16 tokens: what the tokens' own factors are off by does not
-// add up beyond their tile, and states that do not decay, or by less than 32 bits can tell a token, are held.
-// 1e-8 more in the exponent makes up for the mean (2^0 stays 1).
+// 0.12 2^-24 on average there (a million arguments from -1e-2 to -1e-5; no more than 0.7 2^-24 at any).  So a state goes over a block of
+// tokens (a tile, or the 32 or 64 that are staged together) by the factor of the block, e^(A sum of deltas), one exponential for them all:
+// what the tokens' own factors are off by does not add up beyond their block, and states that do not decay, or by less than 32 bits can
+// tell for a token, are held.  1e-8 more in the exponent makes up for the mean (2^0 stays 1).
 __device__ __forceinline__ float factor_of(float delta, float A) { return exp2_of(fmaf(delta, A, 1e-8f)); }
 // the sum of the 16 lanes of a row, the same bits in all of them
 template <int N>
 __device__ __forceinline__ float add_rotated(float v) {
   return v + __int_as_float(__builtin_amdgcn_mov_dpp(__float_as_int(v), 0x120 + N, 0xf, 0xf, true));
 }
-// a tile's sum of deltas, bounded: of steps near the largest number it would be infinite, and NaN times an A of 0
+// the sum of a block's deltas, bounded: of steps near the largest number it would be infinite, and NaN times an A of 0
 __device__ __forceinline__ float sum_of_row(float delta) {
   return add_rotated<1>(add_rotated<2>(add_rotated<4>(add_rotated<8>(__builtin_amdgcn_fmed3f(delta, -1e37f, 1e37f)))));
 }
-// What is to be added to a state behind a tile that began with `before` and was multiplied by `product` where `factor` is right.
-// (An infinite state is infinite behind the tile too; its difference of factors may be 0.)
+// What is to be added to a state behind a block that began with `before` and was multiplied by `product` where `factor` is right.
+// (An infinite state is infinite behind the block too; its difference of factors may be 0.)
 __device__ __forceinline__ float put_right(float factor, float product, float before) {
   return (factor - product) * __builtin_amdgcn_fmed3f(before, -3e38f, 3e38f);
 }

@@ -9,8 +9,9 @@
 // De-composition.  A row of 16 lanes is a channel, a lane one state of every 16; a wavefront has four channels, a workgroup 8 or 16.
 // Tokens are walked in tiles of 16.  Lane j loads x, dt and gate of token j, takes the softplus, and a step's delta reaches the row's
 // other lanes as a modifier of the multiplication.  c_t . h_t: every lane's term goes to LDS, lane j adds up token j's.
-// b and c of a tile lie in LDS as fp32.  A state goes over a tile by the tile's own factor (mdh_selective.h): in turn that is another
-// multiplication a step, the product of the factors that it went by (32768 tokens of 1536 channels 486 us, so 506).  With too few channels for the chip, tokens are cut into segments: what each leaves from
+// b and c of a tile lie in LDS as fp32.  A state goes over a block of tokens by the block's own factor (mdh_selective.h): in turn that is
+// another multiplication a step, the product of the factors that it went by (32768 tokens of 1536 channels 487 us, so 497; tile by tile
+// 507).  With too few channels for the chip, tokens are cut into segments: what each leaves from
 // a state of zeros and the sum of its deltas (its decay is e^(A sum)), a prefix sum over the segments, the pass itself.
 #include "mdh_selective.h"
 
@@ -41,7 +42,7 @@ using ManyAtOnce = Form<NS, 8, 8, 128>;
 
 // STATES_ONLY: a segment's own state and sum of deltas.  Else the pass.
 template <typename T, int NS, typename F, bool STATES_ONLY>
-__global__ __launch_bounds__(F::THREADS, NS == 4 ? 3 : 1) void scan_kernel(ScanCall c, Segments segs, int blocks) {
+__global__ __launch_bounds__(F::THREADS, NS == 4 && sizeof(T) == 4 ? 3 : 1) void scan_kernel(ScanCall c, Segments segs, int blocks) {
   constexpr int S = NS * 16, CH = F::CH, W = F::W, TOKENS = F::TOKENS, NA = STATES_ONLY ? 2 : 3, NB = STATES_ONLY ? 1 : 2;
   typedef Stage<T, NA, NB, CH, S, TOKENS, F::THREADS> In;
   typedef Outputs<T, 1, CH, TOKENS, F::THREADS> Out;
@@ -101,11 +102,16 @@ __global__ __launch_bounds__(F::THREADS, NS == 4 ? 3 : 1) void scan_kernel(ScanC
     T *const xs = raw, *const dts = raw + TOKENS * CH, *const gates = raw + 2 * TOKENS * CH;
     const bool more = t0 + TOKENS < p.alive;
     const int tokens = (int)min((int64_t)TOKENS, p.alive - t0);
+    // in turn: of the block, what it begins with, the product of its factors, a lane's share of its deltas
+    float before[NS], all[NS], sum = 0.f;
+    if constexpr (W == 1)
+#pragma unroll
+      for (int s = 0; s < NS; ++s) before[s] = h[s], all[s] = 1.f, h[s] = STATES_ONLY ? 0.f : h[s];
     for (int i0 = tile * kTile; i0 < (W > 1 ? (tile + 1) * kTile : tokens); i0 += kTile) {
       const int at = place_of<T, CH>(i0 + p.j, p.row);
       const bool live = i0 + p.j < tokens;
       const Token k = token_of(c, to_float(xs[at]), to_float(dts[at]), live, dt_bias);
-      const float u = k.delta * k.x, sum = sum_of_row(k.delta);
+      const float u = k.delta * k.x;
       total += k.delta;
       float y[kTile];
       const float* bs = bc + p.j * In::kPitch + i0;
@@ -113,9 +119,6 @@ __global__ __launch_bounds__(F::THREADS, NS == 4 ? 3 : 1) void scan_kernel(ScanC
         keep(t0 + i0, h);
 #pragma unroll
         for (int s = 0; s < NS; ++s) {
-          const float before = h[s];
-          float all = 1.f;
-          if (STATES_ONLY) h[s] = 0.f;
           unroll<kTile / 4>([&](auto quarter) {
             constexpr int Q = decltype(quarter)::value * 4;
             const Float4 bt = four_of(bs + s * 16 * In::kPitch + Q), ct = four_of(bs + (STATES_ONLY ? 0 : In::kFloats) + s * 16 * In::kPitch + Q);
@@ -123,19 +126,15 @@ __global__ __launch_bounds__(F::THREADS, NS == 4 ? 3 : 1) void scan_kernel(ScanC
               constexpr int I = decltype(i)::value;
               const float a = exp2_of(lane_of_row<Q + I>(k.delta) * A[s]);
               h[s] = fmaf(a, h[s], lane_of_row<Q + I>(u) * bt[I]);
-              if (!STATES_ONLY) all *= a, y[Q + I] = s ? fmaf(ct[I], h[s], y[Q + I]) : ct[I] * h[s];
+              if (!STATES_ONLY) all[s] *= a, y[Q + I] = s ? fmaf(ct[I], h[s], y[Q + I]) : ct[I] * h[s];
             });
           });
-          const float factor = factor_of(sum, A[s]);
-          if (STATES_ONLY) {
-            h[s] = fmaf(factor, before, h[s]);
-          } else {
-            h[s] += put_right(factor, all, before);
-            if (NS == 4) settle(h[s]);  // (one block of states after the other: all at once take 191 registers for 149)
-          }
+          if (!STATES_ONLY) settle(all[s]);  // (one block of states after the other: all at once take up to 40 registers more)
         }
+        sum += k.delta;
       } else {
         float own[NS][kTile], product[NS][kTile];
+        const float deltas = sum_of_row(k.delta);
 #pragma unroll
         for (int s = 0; s < NS; ++s) {
           float from_zero = 0.f, all = 1.f;
@@ -150,10 +149,9 @@ __global__ __launch_bounds__(F::THREADS, NS == 4 ? 3 : 1) void scan_kernel(ScanC
               own[s][Q + I] = from_zero, product[s][Q + I] = all;
             });
           });
-          ends[tile][(s * CH + p.row) * 16 + p.j] = make_float2(from_zero, factor_of(sum, A[s]));
+          ends[tile][(s * CH + p.row) * 16 + p.j] = make_float2(from_zero, factor_of(deltas, A[s]));
         }
         __syncthreads();
-        float before[NS];
 #pragma unroll
         for (int s = 0; s < NS; ++s) {
           before[s] = h[s];
@@ -188,6 +186,14 @@ __global__ __launch_bounds__(F::THREADS, NS == 4 ? 3 : 1) void scan_kernel(ScanC
           v *= g * sigmoid(g);
         }
         xs[at] = from_float<T>(live ? v : 0.f);  // where x was
+      }
+    }
+    if constexpr (W == 1) {
+      const float deltas = sum_of_row(sum);
+#pragma unroll
+      for (int s = 0; s < NS; ++s) {
+        const float factor = factor_of(deltas, A[s]);
+        h[s] = STATES_ONLY ? fmaf(factor, before[s], h[s]) : h[s] + put_right(factor, all[s], before[s]);
       }
     }
     if (BUFFERS == 2) turn ^= 1;

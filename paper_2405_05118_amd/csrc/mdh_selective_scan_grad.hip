@@ -2,7 +2,8 @@
 //   G_t = E_t + d_p c_t,  E_{t-1} = a_t G_t;   d_c = sum_d d_p h_t,  d_b = sum_d G_t delta x,  r = sum_n G_t b_t,  q = G_t a_t h_{t-1}
 //   d_x = delta r + skip d_p,  d_delta = sum_n q A + x r,  d_A = sum_t q delta,  d_skip = sum d_p x,  d_gate = d_y p silu'(gate)
 // from the last token to the first.  The states h come from the forward call's checkpoints, one for every tile of 16 tokens:
-// a tile's a_t and h_t are computed again and stay in registers while it is walked back; E goes over the tile by the tile's own factor.
+// a tile's a_t and h_t are computed again and stay in registers while it is walked back; E goes over a block
+// of 32 tokens by the block's own factor.
 //
 // 1 exponential and 15 multiplications a step: bound by the vector ALU (26 of its instructions a step, sums and staging with them).
 // 4 x 2048 tokens of 4096 channels with 16 states, bf16: 516 to 565 us in a kernel trace, 26 for the sums of d_b and d_c.
@@ -166,6 +167,10 @@ __global__ __launch_bounds__(64 * WAVES, NS == 1 && sizeof(T) == 2 ? 4 : 2) void
     behind = true;
     if (t0 > p.first) load(t0 - kTokens);
     const int tokens = (int)min((int64_t)kTokens, p.alive - t0);
+    // of the block: what it is walked back from, the product of its factors, a lane's share of its deltas
+    float behind_it[NS], all[NS], deltas = 0.f;
+#pragma unroll
+    for (int s = 0; s < NS; ++s) behind_it[s] = e[s], all[s] = 1.f;
 #pragma unroll
     for (int tile = TILES - 1; tile >= 0; --tile) {
       const int i0 = tile * kTile;
@@ -174,13 +179,13 @@ __global__ __launch_bounds__(64 * WAVES, NS == 1 && sizeof(T) == 2 ? 4 : 2) void
       const int at = place_of<T, CH>(i0 + p.j, p.row);
       const Token k = token_of(c, to_float(xs[at]), to_float(dts[at]), live, dt_bias);
       const float dy = to_float(dys[at]), dp = c.in[2].p ? dy * gate_of(to_float(gates[at])) : dy, u = k.delta * k.x;
-      const float delta_sum = sum_of_row(k.delta);
+      deltas += k.delta;
       float sp = 0.f, sr = 0.f, sq = 0.f;
       float* own = sums[wave];
 #pragma unroll
       for (int s = 0; s < NS; ++s) {
         const float* bs = bc + (s * 16 + p.j) * In::kPitch + i0;
-        float h[kTile + 1], a[kTile], g[kTile], all = 1.f;
+        float h[kTile + 1], a[kTile], g[kTile];
         h[0] = h0[tile][s];
         unroll<kTile / 4>([&](auto quarter) {
           constexpr int Q = decltype(quarter)::value * 4;
@@ -188,13 +193,12 @@ __global__ __launch_bounds__(64 * WAVES, NS == 1 && sizeof(T) == 2 ? 4 : 2) void
           unroll<4>([&](auto i) {
             constexpr int I = Q + decltype(i)::value;
             a[I] = exp2_of(lane_of_row<I>(k.delta) * A[s]);
-            all *= a[I];
+            all[s] *= a[I];
             h[I + 1] = fmaf(a[I], h[I], lane_of_row<I>(u) * bt[I - Q]);
             own[I * kSumPitch + lane] = ct[I - Q] * h[I + 1];
           });
         });
-        float right = put_right(factor_of(delta_sum, A[s]), all, e[s]);
-        settle(right);
+        settle(all[s]);
         wave_fence();
         sp += row_sum(own, lane);
         settle(sp);
@@ -225,7 +229,6 @@ __global__ __launch_bounds__(64 * WAVES, NS == 1 && sizeof(T) == 2 ? 4 : 2) void
             add_lane_of_row<I>(dA[s], delta2, a[I]);
           });
         });
-        e[s] += right;
         wave_fence();
         sr += row_sum(own, lane);
         settle(sr), settle(dA[s]), settle(e[s]);
@@ -262,6 +265,9 @@ __global__ __launch_bounds__(64 * WAVES, NS == 1 && sizeof(T) == 2 ? 4 : 2) void
         gates[at] = from_float<T>(live ? dy * fmaf(skip, k.x, sp) * f * (1.f + g * (1.f - f)) : 0.f);
       }
     }
+    deltas = sum_of_row(deltas);
+#pragma unroll
+    for (int s = 0; s < NS; ++s) e[s] += put_right(factor_of(deltas, A[s]), all[s], behind_it[s]);
     __syncthreads();
   }
   if (behind) {
