@@ -273,9 +273,10 @@ __global__ __launch_bounds__(256) void scan_step_kernel(ScanCall c, unsigned blo
         bt[0] = to_float(*pb), ct[0] = to_float(*pc);
       }
       const Token k = token_of(c, x, dt, true, c.dt_bias ? c.dt_bias[d] : 0.f);
+      const float steps = __builtin_amdgcn_fmed3f(k.delta * kLog2e, -3.4e38f, 3.4e38f);  // (infinite, it would make NaN of an A of 0)
 #pragma unroll
       for (int s = 0; s < V; ++s) {
-        h[s] = fmaf(factor_of(k.delta, in_powers_of_2(A[s])), h[s], k.delta * k.x * bt[s]);
+        h[s] = fmaf(factor_of(steps, A[s]), h[s], k.delta * k.x * bt[s]);
         y = fmaf(ct[s], h[s], y);
       }
       *(fv*)state = h;
