@@ -276,7 +276,7 @@ __global__ __launch_bounds__(kThreads) void conv_step_kernel(ConvCall c, Grid g)
 }
 
 enum Which { kForward, kBackward, kStep };
-// Channels of a lane.  (8 of bf16, which are 16 bytes, hold twice the filters: 103 registers become 164 and more, 6 x 1021 x 2500
+// Channels of a lane.  (8 of bf16, which are 16 bytes, hold twice the filters: then 103 registers became 164 and more, 6 x 1021 x 2500
 // 16.6 us become 30, 4 x 2048 x 4096 33 become 34.)
 constexpr int kValues = 4;
 

@@ -4,14 +4,14 @@
 // 1 exponential and 4 multiplications a step (token, channel, state), on 8 bytes a token and channel (bf16, N = 16): bound by the
 // vector ALU.  Measured on this chip, cycles of a wavefront instruction with four wavefronts a SIMD: v_exp_f32 8.4, fma and
 // multiplication 2.6 to 3.2, with a lane of the row broadcast to it (DPP) 4.4; a step of all of them 24 to 27 (with two wavefronts 31,
-// with one 57).  Times (bf16, N = 16): 2048 tokens of 4096 channels 81 us; 32768 tokens of 1536 channels 474 us.
+// with one 57).  Times (bf16, N = 16): 2048 tokens of 4096 channels 81 us; 32768 tokens of 1536 channels 492 us.
 //
 // De-composition.  A row of 16 lanes is a channel, a lane one state of every 16; a wavefront has four channels, a workgroup 8 or 16.
 // Tokens are walked in tiles of 16.  Lane j loads x, dt and gate of token j, takes the softplus, and a step's delta reaches the row's
 // other lanes as a modifier of the multiplication.  c_t . h_t: every lane's term goes to LDS, lane j adds up token j's.
 // b and c of a tile lie in LDS as fp32.  A state goes over a block of tokens by the block's own factor (mdh_selective.h): in turn that is
-// another multiplication a step, the product of the factors that it went by (32768 tokens of 1536 channels 487 us, so 497; tile by tile
-// 507).  With too few channels for the chip, tokens are cut into segments: what each leaves from
+// another multiplication a step, the product of the factors that it went by (4 x 2048 tokens of 4096 channels 205 us, so 215; tile by
+// tile 219).  With too few channels for the chip, tokens are cut into segments: what each leaves from
 // a state of zeros and the sum of its deltas (its decay is e^(A sum)), a prefix sum over the segments, the pass itself.
 #include "mdh_selective.h"
 
@@ -301,9 +301,9 @@ struct Plan {
   int64_t tokens;  // of a segment
 };
 // The least of estimated times, in cycles for 16 states.  In turn: 55 a token and 60 for every wavefront of a SIMD (one of them: 2048
-// tokens of 4096 channels 116 us; four: 4 x 2048 of 4096 234).  At once: 98 a token with two workgroups of 8 wavefronts a compute unit,
-// 65 with one (84 us), 60 with one of 16 (32768 of 1536 channels: 826).  Segments: 92 a step whatever the shape, and two more launches
-// (32768 of 1536: 474; 2048 of 4096: 99), 15 us in all.
+// tokens of 4096 channels 118 us; four: 4 x 2048 of 4096 216).  At once: 98 a token with two workgroups of 8 wavefronts a compute unit
+// (2048 of 4096: 82), 65 with one (2048 of 2048: 56), 60 with one of 16 (32768 of 1536: 853).  Segments: 92 a step whatever the shape, and two more launches
+// (32768 of 1536: 492; 2048 of 4096: 105), 15 us in all.
 Plan plan(const ScanCall& c) {
   const int ns = states_of(c);
   const int64_t T = c.T, eights = c.B * c.G * cdiv(c.E, 8), groups = c.B * c.G * cdiv(c.E, 16);

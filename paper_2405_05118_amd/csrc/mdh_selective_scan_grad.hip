@@ -5,8 +5,8 @@
 // a tile's a_t and h_t are computed again and stay in registers while it is walked back; E goes over a block
 // of 32 tokens by the block's own factor.
 //
-// 1 exponential and 15 multiplications a step: bound by the vector ALU (26 of its instructions a step, sums and staging with them).
-// 4 x 2048 tokens of 4096 channels with 16 states, bf16: 516 to 565 us in a kernel trace, 26 for the sums of d_b and d_c.
+// 1 exponential and 16 multiplications a step: bound by the vector ALU (28 of its instructions a step, sums and staging with them).
+// 4 x 2048 tokens of 4096 channels with 16 states, bf16: 546 us, 557 to 586 in a kernel trace, 26 for the sums of d_b and d_c.
 // De-composition as in the forward pass (a row of 16 lanes is a channel, a lane a state); a workgroup has 32 channels.  Sums over the
 // states (p, r, sum q A) go through LDS, token j's to lane j.  Sums over the channels (d_b, d_c): rows of the wavefront exchange halves, then
 // LDS over the workgroup's wavefronts, in two places by turns: one barrier a tile (with all five sums through LDS and two barriers 721

@@ -86,7 +86,8 @@ class SelectiveLayer:
 
     def forward(self, x, stream, out, lengths=None):
         """x, stream, out: (batch, length, width); returns (out, the stream with x added, a buffer of the layer).  States and windows
-        begin at zero and are left as they are after every sequence's last token (``lengths`` (batch,) int32: after that many)."""
+        begin at zero and are left as they are after every sequence's last token (``lengths`` (batch,) int32: after that many.  What
+        x and the stream hold behind them goes through norm and projections like any row: finite, where gradients are wanted)."""
         B, T, C, w, ws = self.batch, self.length, self.channels, self.weights, self.workspace
         rows = x.view(B * T, -1)
         self._norm(rows, stream.view(B * T, -1), self.total, self.n, self.mean, self.rstd)
