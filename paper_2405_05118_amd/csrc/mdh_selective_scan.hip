@@ -303,7 +303,9 @@ struct Plan {
 // The least of estimated times, in cycles for 16 states.  In turn: 55 a token and 60 for every wavefront of a SIMD (one of them: 2048
 // tokens of 4096 channels 118 us; four: 4 x 2048 of 4096 216).  At once: 98 a token with two workgroups of 8 wavefronts a compute unit
 // (2048 of 4096: 82), 65 with one (2048 of 2048: 56), 60 with one of 16 (32768 of 1536: 853).  Segments: 92 a step whatever the shape, and two more launches
-// (32768 of 1536: 492; 2048 of 4096: 105), 15 us in all.
+// (32768 of 1536: 492; 2048 of 4096: 105), 15 us in all.  Where that misses: more than 16 states are more cycles a token, of which the rule
+// knows nothing (300 tokens of 1024 channels with 64 states go in turn, 42 us; segments 29); 2048 of 1536 and 8192 of 4096 go in segments (57
+// and 334; at once 47 and 292).
 Plan plan(const ScanCall& c) {
   const int ns = states_of(c);
   const int64_t T = c.T, eights = c.B * c.G * cdiv(c.E, 8), groups = c.B * c.G * cdiv(c.E, 16);
