@@ -182,9 +182,12 @@ def main(argv=None):
         d_stream = d_out = d_y  # both reach the sum behind the last layer
         for layer in reversed(whole):
             d_stream = d_out = layer.backward(d_out, d_stream, d_x).clone()
+        # steps of length 0.1 at most: a scan's gradients grow with the cube of what goes in, and longer ones end in NaN
+        size = sum(float(grad.square().sum()) for layer in whole for grad in layer.grads.values()) ** 0.5
         for layer in whole:
             for name, grad in layer.grads.items():
-                layer.weights[name].add_(grad, alpha=-0.1)
+                layer.weights[name].add_(grad, alpha=-0.1 / max(1.0, size))
+            layer.weights["A"].clamp_(max=-1e-3)  # (states that grow are not the scan's)
     if a.steps:
         print("%d steps of training: mean squared error %.4f -> %.4f" % (a.steps, first, loss))
     return off, first, loss

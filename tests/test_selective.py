@@ -161,6 +161,16 @@ def test_command(capsys):
     assert "tokens after a prompt" in capsys.readouterr().out
 
 
+@gpu
+@pytest.mark.parametrize("seed", [0, 1, 2])
+def test_command_as_it_is(seed):
+    """The command's own sizes and steps: numbers to the end."""
+    from paper_2405_05118_amd import selective
+
+    off, first, loss = selective.main(["--seed", str(seed)])
+    assert off <= LIMIT and np.isfinite(first) and np.isfinite(loss)
+
+
 def test_channels_that_do_not_fall_into_groups_are_refused():
     from paper_2405_05118_amd.selective import SelectiveLayer
 
